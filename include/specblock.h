@@ -20,6 +20,12 @@
  *   sb_kv_compact      move the accepted path's K/V behind the prefix   (Sec. 3.1, App. A.2: committed positions stay in the cache)
  *   sb_path_rows       the accepted path in the drafter's row numbering  (App. A.2)
  *
+ * and the same steps over a cache held in 8 bits, with the pages that hold a cache:
+ *
+ *   sb_tree_attention_quant  tree attention over an e4m3 prefix, sliding window and sinks
+ *   sb_kv_append_quant       prompt rows or the accepted path become codes and scales
+ *   sb_pages_fork / _reserve / _release / _compact / _copy   pages shared between sequences
+ *
  * Conventions that hold for every call
  *   - Every pointer is a DEVICE pointer owned by the caller unless its comment says "host".
  *     The library never allocates or frees device memory, enqueues its kernels on `stream` (a
@@ -66,7 +72,8 @@ typedef enum sb_status {
   SB_ERR_WORKSPACE = 3,    /* workspace smaller than the *_workspace_bytes query         */
   SB_ERR_INVALID_TREE = 4, /* per-sequence: parent[i] not in {-1} U [0,i), too many nodes */
   SB_ERR_BOUNDS = 5,       /* per-sequence: prefix+nodes beyond cache, page id outside pool */
-  SB_ERR_CUDA = 6          /* a CUDA runtime call or launch failed                       */
+  SB_ERR_CUDA = 6,         /* a CUDA runtime call or launch failed                       */
+  SB_ERR_NO_PAGES = 7      /* sb_pages_reserve: the pool has too few free pages          */
 } sb_status;
 
 typedef enum sb_dtype { SB_BF16 = 0, SB_F32 = 1 } sb_dtype;
@@ -454,6 +461,179 @@ sb_status sb_kv_compact(const sb_tree_batch* tb, int32_t n_layers, int64_t layer
 sb_status sb_path_rows(int32_t batch, const int32_t* node_offsets, const int32_t* node_row,
                        const int32_t* row_begin, const int32_t* path_nodes, const int32_t* accept_len,
                        int32_t max_depth, int32_t* path_rows, int32_t* status, void* stream);
+
+/*
+ * A KV cache held in 8 bits: e4m3 codes with one fp32 scale for each block of scale_block consecutive
+ * tokens and each KV head.  value = code * scale.  (The paper has no counterpart; the layouts are those of
+ * the bf16 caches above with one byte per element.)
+ *   codes  : page_size == 0  [batch][kv_capacity][n_kv_heads][head_dim], kv_capacity a multiple of scale_block
+ *            page_size  > 0  [num_pages][page_size][n_kv_heads][head_dim], page_size a multiple of scale_block
+ *   scales : [tokens of the cache / scale_block][n_kv_heads], the blocks in the order of the codes' rows
+ *   n_layers layers, codes_layer_stride elements and scale_layer_stride scales apart.
+ * sb_kv_append_quant writes powers of two; the attention takes any positive scale up to 2^40.  A V scale
+ * below 2^-60 reads as a block of zeros; a NaN scale marks a block that was written from a NaN or an infinity:
+ * every node that sees one of its tokens gets NaN.  Codes are finite (0x7F and 0xFF, e4m3's NaN, are
+ * never written and must not occur in a visible row).
+ */
+typedef struct sb_quant_cache {
+  int32_t batch;       /* sequences                                                  */
+  int32_t n_kv_heads;
+  int32_t head_dim;    /* 64 or 128                                                  */
+  int32_t scale_block; /* 16, 32, 64 or 128 tokens                                   */
+  void* k_codes;       /* 16-byte aligned                                            */
+  void* v_codes;
+  float* k_scale;
+  float* v_scale;
+  int32_t page_size;   /* 0 = contiguous, else a power of two >= 16                  */
+  int32_t max_pages;   /* paged: row length of page_table                            */
+  int64_t kv_capacity; /* contiguous: positions per sequence                         */
+  int32_t num_pages;   /* paged: pages in the pool                                   */
+  int32_t n_layers;
+  int64_t codes_layer_stride; /* bytes, a multiple of 16                             */
+  int64_t scale_layer_stride; /* floats                                              */
+  const int32_t* page_table;  /* [batch][max_pages], paged only                      */
+} sb_quant_cache;
+
+/* The ragged batch of draft trees that attends to such a cache; arrays as in sb_tree_batch. */
+typedef struct sb_quant_tree {
+  int32_t n_q_heads;   /* Hq, a multiple of n_kv_heads, at most 16 times it          */
+  int32_t total_nodes; /* host copy of node_offsets[batch]                           */
+  int32_t max_nodes;   /* host upper bound on N_b (<= SB_MAX_NODES)                  */
+  int32_t max_prefix;  /* host upper bound on P_b                                    */
+  const int32_t* prefix_len;   /* [batch]  P_b >= 0, committed tokens in the cache   */
+  const int32_t* node_offsets; /* [batch+1]                                          */
+  const int32_t* parent;       /* [total_nodes]                                      */
+} sb_quant_tree;
+
+/*
+ * sb_tree_attention_quant -- tree-masked attention of one layer over an 8-bit prefix.
+ *
+ *   The prefix is read from the cache; the tree's own keys and values are the bf16 rows its forward has just
+ *   produced, k_nodes / v_nodes [total_nodes][n_kv_heads][head_dim] with node_stride elements between rows
+ *   (a slice of a fused projection; 0 = n_kv_heads * head_dim).  They are not in the cache: sb_kv_append_quant
+ *   commits the accepted ones.  A single token per sequence is a tree of one node.
+ *
+ *   Node i of depth d sits at position P + d.  It sees prefix position j iff j < sinks or P + d - j < window,
+ *   and its ancestor a (itself included) iff P + depth(a) < sinks or d - depth(a) < window.  window = 0 (then
+ *   sinks must be 0): no window.  A key block that no node can see is not read.
+ *
+ *   q bf16 [total_q][Hq][D], q_stride elements between rows (0 = Hq * D); out, lse, scale, num_splits,
+ *   q_node_begin, q_offsets and status as for sb_tree_attention.  q_stride and node_stride are multiples of 8,
+ *   q, k_nodes, v_nodes and out 16-byte aligned.  `layer` picks one of the cache's layers.
+ *   A node row of K or V that holds a NaN or an infinity makes the outputs of the nodes that see it NaN and
+ *   changes no other node's.  Scores, softmax and outputs are accumulated in fp32; Q (scaled by a power of two
+ *   per row), the codes and the probabilities enter the products as fp16 (node rows: fp16 with a power of two
+ *   per 16 nodes, or bf16).
+ *   workspace: sb_tree_attention_quant_workspace_bytes(...) bytes, 256-byte aligned, no initialisation; calls
+ *   that may overlap on the GPU need distinct workspaces.
+ */
+sb_status sb_tree_attention_quant(const sb_quant_cache* kv, int32_t layer, const sb_quant_tree* tree,
+                                  const void* k_nodes, const void* v_nodes, int64_t node_stride,
+                                  const int32_t* q_node_begin, const int32_t* q_offsets, int32_t total_q,
+                                  const void* q, int64_t q_stride, void* out, float* lse, float scale,
+                                  int32_t window, int32_t sinks, int32_t num_splits, void* workspace,
+                                  size_t workspace_bytes, int32_t* status, void* stream);
+size_t sb_tree_attention_quant_workspace_bytes(const sb_quant_cache* kv, const sb_quant_tree* tree,
+                                               int32_t total_q, int32_t window, int32_t sinks,
+                                               int32_t num_splits);
+
+/*
+ * sb_kv_append_quant -- bf16 rows become the next tokens of an 8-bit cache, all layers in one call.
+ *
+ *   k_rows / v_rows bf16: row r of layer l starts l * rows_layer_stride + r * row_stride elements in and
+ *   holds [n_kv_heads][head_dim] (row_stride 0 = n_kv_heads * head_dim).  Sequence b appends at position len[b]:
+ *     path_nodes == NULL : rows row_offsets[b] .. row_offsets[b+1] - 1 (a prompt, or a piece of one);
+ *     else               : rows row_offsets[b] + path_nodes[b][j], j = 0 .. accept_len[b] (the accepted path,
+ *                          both arrays as sb_verify_accept leaves them, row length max_depth + 1).
+ *   For every block of tokens and head that receives rows: s = the smallest power of two, at least 2^-100,
+ *   with max |x| <= 448 s over the new rows; if the block holds older tokens, s = max(s, old scale) and their
+ *   codes become round(code * old / s).  New codes are round(x / s).  Rounding is to the nearest e4m3 value, ties to
+ *   even.  A NaN or an infinity makes the block's scale NaN (its code is 0).  Bytes and scales of tokens
+ *   past the appended ones, and of other blocks, stay as they are.
+ *   new_len[b] = len[b] + the rows appended.  new_len is a distinct array from len.
+ *   max_rows: host upper bound on the rows of a sequence.  total_rows: host copy of row_offsets[batch].
+ *   status int32 [batch]: SB_ERR_INVALID_TREE (offsets or path out of order), SB_ERR_BOUNDS (past the capacity, or
+ *   a page id outside the pool); nothing of such a sequence is written and new_len[b] = len[b].
+ *   Sequences that share the page they append to must not be in one call (sb_pages_reserve gives each its own).
+ */
+sb_status sb_kv_append_quant(const sb_quant_cache* kv, const void* k_rows, const void* v_rows,
+                             int64_t row_stride, int64_t rows_layer_stride, const int32_t* row_offsets,
+                             int32_t total_rows, const int32_t* path_nodes, const int32_t* accept_len,
+                             int32_t max_depth, int32_t max_rows, const int32_t* len, int32_t* new_len,
+                             int32_t* status, void* stream);
+
+/*
+ * Pages of a cache shared between sequences.  A slot is a row of page_table: a sequence's logical pages in
+ * order, held[slot] of them, -1 behind.  refs[page] counts the slots that hold a page; 0 = free.  The
+ * arrays are the caller's; start with page_table = -1, held = refs = 0.  The calls keep them consistent, and every
+ * choice they make follows from the arrays' contents alone (the lowest free page first, in list order), so that equal
+ * states give equal results.  Conventions common to the calls:
+ *   - `slots` and the other lists hold n >= 0 int32 entries (host count n); status int32 [n], per entry.  An
+ *     entry with a slot outside [0, n_slots), or a slot that an earlier entry of the list names, gets
+ *     SB_ERR_INVALID_ARG; an entry whose table is damaged (held > max_pages, a page id outside the pool, a page
+ *     with refs < 1) or whose lengths do not fit gets SB_ERR_BOUNDS.  Such an entry changes nothing; the others
+ *     are served.
+ *   - workspace: sb_pages_workspace_bytes(pool, n) bytes, 256-byte aligned, no initialisation.
+ *   - calls on one pool are ordered by the caller's stream.
+ */
+typedef struct sb_page_pool {
+  int32_t num_pages;
+  int32_t page_size;   /* positions per page, a power of two >= 16                   */
+  int32_t n_slots;
+  int32_t max_pages;   /* row length of page_table                                   */
+  int32_t* page_table; /* [n_slots][max_pages]                                       */
+  int32_t* held;       /* [n_slots]                                                  */
+  int32_t* refs;       /* [num_pages]                                                */
+} sb_page_pool;
+size_t sb_pages_workspace_bytes(const sb_page_pool* pool, int32_t n);
+
+/* sb_pages_fork -- slot dst[i], which holds nothing, shares the pages of src[i] that hold its first len[i]
+ * positions.  src may repeat; a dst that is also a src of the call still holds nothing. */
+sb_status sb_pages_fork(const sb_page_pool* pool, int32_t n, const int32_t* src, const int32_t* dst,
+                        const int32_t* len, void* workspace, size_t workspace_bytes, int32_t* status,
+                        void* stream);
+
+/* sb_pages_reserve -- makes positions [keep_len[i], new_len[i]) of slots[i] writable: pages are added up to new_len,
+ * and a page that holds any of these positions and is shared becomes the slot's own.  When every holder of a
+ * shared page is served by this call the first of them in the list keeps it.  If the
+ * replaced page also holds positions below keep_len (at most one page per slot does) the pair (old page, new
+ * page) is appended to the copy list, for sb_pages_copy to copy the contents.
+ * copy_src / copy_dst int32 [n] (list order, -1 behind the last pair), n_copies int32 [1].
+ * 0 <= keep_len <= new_len <= max_pages * page_size, keep_len within the pages held.  If the free pages do not
+ * suffice for the whole list nothing changes and every entry that asked for a page gets SB_ERR_NO_PAGES. */
+sb_status sb_pages_reserve(const sb_page_pool* pool, int32_t n, const int32_t* slots, const int32_t* keep_len,
+                           const int32_t* new_len, int32_t* copy_src, int32_t* copy_dst, int32_t* n_copies,
+                           void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/* sb_pages_release -- slots[i] keeps the pages of its first keep_len[i] positions and lets the others go; a page
+ * without a holder is free.  keep_len = 0 ends a sequence. */
+sb_status sb_pages_release(const sb_page_pool* pool, int32_t n, const int32_t* slots, const int32_t* keep_len,
+                           void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/* sb_pages_compact -- moves the pages in use to the front of the pool: with U pages in use, the k-th used page
+ * (ascending) at or past U moves to the k-th free page below U.  Tables and refs follow; the copy list tells
+ * sb_pages_copy what to move (sources and destinations are disjoint).  copy_src / copy_dst int32 [max_copies],
+ * max_copies >= num_pages / 2; n_copies, n_used int32 [1] (n_used may be NULL); status int32 [1]:
+ * SB_ERR_BOUNDS when a table is damaged, then nothing changes. */
+sb_status sb_pages_compact(const sb_page_pool* pool, int32_t* copy_src, int32_t* copy_dst, int32_t max_copies,
+                           int32_t* n_copies, int32_t* n_used, void* workspace, size_t workspace_bytes,
+                           int32_t* status, void* stream);
+
+/* One array that is cut into pages: page p of layer l starts at base + l * layer_stride + p * page_bytes. */
+typedef struct sb_page_array {
+  void* base;           /* page_bytes and layer_stride multiples of 4, base 4-byte aligned */
+  int64_t page_bytes;
+  int64_t layer_stride; /* bytes                                                      */
+} sb_page_array;
+#define SB_MAX_PAGE_ARRAYS 8
+
+/* sb_pages_copy -- page copy_dst[i] <- page copy_src[i], i < *n_copies, in every layer of every array (K and V
+ * codes and scales of an 8-bit cache, or K and V of a bf16 one), one launch.  `arrays` is a host array.  No page is
+ * both a source and a destination, and no destination occurs twice.  At most max_copies pairs are read; pairs
+ * with an id outside [0, num_pages) are skipped. */
+sb_status sb_pages_copy(const sb_page_array* arrays, int32_t n_arrays, int32_t n_layers, int32_t num_pages,
+                        const int32_t* copy_src, const int32_t* copy_dst, const int32_t* n_copies,
+                        int32_t max_copies, void* stream);
 
 /* Text for a status code (static storage). */
 const char* sb_status_string(sb_status s);

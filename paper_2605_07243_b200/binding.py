@@ -23,7 +23,7 @@ SB_KMAX = 16
 SB_BF16, SB_F32 = 0, 1
 
 STATUS_NAMES = {0: "SB_OK", 1: "SB_ERR_INVALID_ARG", 2: "SB_ERR_UNSUPPORTED", 3: "SB_ERR_WORKSPACE",
-                4: "SB_ERR_INVALID_TREE", 5: "SB_ERR_BOUNDS", 6: "SB_ERR_CUDA"}
+                4: "SB_ERR_INVALID_TREE", 5: "SB_ERR_BOUNDS", 6: "SB_ERR_CUDA", 7: "SB_ERR_NO_PAGES"}
 
 
 class SbError(RuntimeError):
@@ -65,6 +65,20 @@ def _open(path: str):
                  "sb_verify_accept_static", "sb_kv_compact", "sb_path_rows", "sb_rank_features", "sb_verifier_signal",
                  "sb_verify_sample", "sb_shift_project", "sb_fuse_project", "sb_tree_expand_features"):
         getattr(lib, name).restype = C.c_int
+    # the calls over 8-bit caches and pages take plain integers for pointers (declared argument types)
+    P, I, L, Z, F = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float
+    for name, res, args in (
+            ("sb_tree_attention_quant", C.c_int, (P, I, P, P, P, L, P, P, I, P, L, P, P, F, I, I, I, P, Z, P, P)),
+            ("sb_tree_attention_quant_workspace_bytes", Z, (P, P, I, I, I, I)),
+            ("sb_kv_append_quant", C.c_int, (P, P, P, L, L, P, I, P, P, I, I, P, P, P, P)),
+            ("sb_pages_workspace_bytes", Z, (P, I)),
+            ("sb_pages_fork", C.c_int, (P, I, P, P, P, P, Z, P, P)),
+            ("sb_pages_reserve", C.c_int, (P, I, P, P, P, P, P, P, P, Z, P, P)),
+            ("sb_pages_release", C.c_int, (P, I, P, P, P, Z, P, P)),
+            ("sb_pages_compact", C.c_int, (P, P, P, I, P, P, P, Z, P, P)),
+            ("sb_pages_copy", C.c_int, (P, I, I, I, P, P, P, I, P))):
+        fn = getattr(lib, name)
+        fn.restype, fn.argtypes = res, args
     return lib
 
 
@@ -108,7 +122,9 @@ EXPORTED = ("sb_tree_ancestors", "sb_tree_attention", "sb_tree_attention_workspa
             "sb_verify_sample_workspace_bytes", "sb_shift_project", "sb_shift_project_workspace_bytes",
             "sb_fuse_project", "sb_fuse_project_workspace_bytes", "sb_tree_expand_features", "sb_status_string",
             "sb_version",
-            "sb_kernel_launch_count")
+            "sb_kernel_launch_count", "sb_tree_attention_quant", "sb_tree_attention_quant_workspace_bytes",
+            "sb_kv_append_quant", "sb_pages_workspace_bytes", "sb_pages_fork", "sb_pages_reserve", "sb_pages_release",
+            "sb_pages_compact", "sb_pages_copy")
 
 
 def _ptr(t: Optional[torch.Tensor], dtype=None):
@@ -492,6 +508,362 @@ def sb_tree_expand(scores, block_k, bucket, bmap, start_parent, node_budget, tre
         _check(lib.sb_tree_expand_features(*head, _ptr(features, torch.float32), _ptr(child_row, torch.int32),
                                            C.c_int32(row_base), *tail), "sb_tree_expand_features")
     return topk_tok, topk_val, status
+
+
+# ---- a KV cache in 8 bits ----------------------------------------------------------------------------------------------
+
+class _QuantCache(C.Structure):
+    _fields_ = [
+        ("batch", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("scale_block", C.c_int32),
+        ("k_codes", C.c_void_p), ("v_codes", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+        ("page_size", C.c_int32), ("max_pages", C.c_int32), ("kv_capacity", C.c_int64), ("num_pages", C.c_int32),
+        ("n_layers", C.c_int32), ("codes_layer_stride", C.c_int64), ("scale_layer_stride", C.c_int64),
+        ("page_table", C.c_void_p),
+    ]
+
+
+class _QuantTree(C.Structure):
+    _fields_ = [
+        ("n_q_heads", C.c_int32), ("total_nodes", C.c_int32), ("max_nodes", C.c_int32), ("max_prefix", C.c_int32),
+        ("prefix_len", C.c_void_p), ("node_offsets", C.c_void_p), ("parent", C.c_void_p),
+    ]
+
+
+class _PagePool(C.Structure):
+    _fields_ = [
+        ("num_pages", C.c_int32), ("page_size", C.c_int32), ("n_slots", C.c_int32), ("max_pages", C.c_int32),
+        ("page_table", C.c_void_p), ("held", C.c_void_p), ("refs", C.c_void_p),
+    ]
+
+
+class _PageArray(C.Structure):
+    _fields_ = [("base", C.c_void_p), ("page_bytes", C.c_int64), ("layer_stride", C.c_int64)]
+
+
+def _addr(t, dtype, device, numel=None):
+    """Address of a contiguous tensor of this type on this device (None: a null pointer)."""
+    if t is None:
+        return None
+    if t.dtype != dtype:
+        raise TypeError(f"expected {dtype}, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"expected a tensor on {device}, got {t.device}")
+    if not t.is_contiguous():
+        raise ValueError("expected a contiguous tensor")
+    if numel is not None and t.numel() != numel:
+        raise ValueError(f"expected {numel} elements, got {tuple(t.shape)}")
+    return t.data_ptr()
+
+
+def _cuda_device(t):
+    """The tensor's device, which has to be the current one: the library enqueues on the current device's stream."""
+    if not t.is_cuda:
+        raise ValueError("expected a CUDA tensor")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return t.device
+
+
+def _stream_of(device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+@dataclass(frozen=True)
+class QuantCache:
+    """A KV cache held as e4m3 codes with one fp32 scale for each block of scale_block tokens and KV head; mirrors the C
+    struct sb_quant_cache.  k_codes / v_codes: uint8 or float8_e4m3fn, contiguous, [(layers,) batch, capacity, Hkv, D], or
+    paged [(layers,) pages, page_size, Hkv, D] with page_table int32 [batch, max_pages].  k_scale / v_scale: fp32
+    [(layers,) batch, capacity / scale_block, Hkv] or [(layers,) pages, page_size / scale_block, Hkv].  The tensors'
+    contents may change between calls; another tensor takes another QuantCache."""
+    k_codes: torch.Tensor
+    v_codes: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+    n_kv_heads: int
+    head_dim: int
+    scale_block: int
+    page_size: int = 0
+    page_table: Optional[torch.Tensor] = None
+    n_layers: int = 1
+
+    def __post_init__(self):
+        s = _QuantCache()
+        dev = self.k_codes.device
+        lead = self.k_codes.shape[:-2]
+        if self.k_codes.dim() != (4 if self.n_layers == 1 and self.k_codes.dim() == 4 else 5):
+            raise ValueError("codes must be [(layers,) rows, tokens, n_kv_heads, head_dim]")
+        if tuple(self.k_codes.shape[-2:]) != (self.n_kv_heads, self.head_dim) or self.v_codes.shape != self.k_codes.shape:
+            raise ValueError("k_codes and v_codes must both end in [n_kv_heads, head_dim]")
+        if len(lead) == 3 and lead[0] != self.n_layers:
+            raise ValueError("the codes' first dimension must be n_layers")
+        rows, tokens = lead[-2:]
+        if self.scale_block < 1 or tokens % self.scale_block:
+            raise ValueError("the tokens of a page (or of a contiguous sequence) must be a multiple of scale_block")
+        scales = self.n_layers * rows * (tokens // self.scale_block) * self.n_kv_heads
+        for name, t in (("k_codes", self.k_codes), ("v_codes", self.v_codes)):
+            if t.dtype not in (torch.uint8, torch.float8_e4m3fn):
+                raise TypeError(f"{name}: expected uint8 or float8_e4m3fn, got {t.dtype}")
+            setattr(s, name, _addr(t, t.dtype, dev))
+        s.k_scale = _addr(self.k_scale, torch.float32, dev, scales)
+        s.v_scale = _addr(self.v_scale, torch.float32, dev, scales)
+        s.n_kv_heads, s.head_dim, s.scale_block = self.n_kv_heads, self.head_dim, self.scale_block
+        s.page_size, s.n_layers = self.page_size, self.n_layers
+        s.codes_layer_stride = self.k_codes.numel() // self.n_layers
+        s.scale_layer_stride = scales // self.n_layers
+        if self.page_size:
+            if tokens != self.page_size or self.page_table is None or self.page_table.dim() != 2:
+                raise ValueError("a paged cache needs codes of page_size tokens a page and a page_table [batch, max_pages]")
+            s.batch, s.max_pages = self.page_table.shape
+            s.num_pages, s.kv_capacity = rows, 0
+            s.page_table = _addr(self.page_table, torch.int32, dev)
+        else:
+            s.batch, s.kv_capacity, s.max_pages, s.num_pages = rows, tokens, 0, 0
+        object.__setattr__(self, "c_struct", s)
+        object.__setattr__(self, "c_ref", C.addressof(s))
+        object.__setattr__(self, "batch", int(s.batch))
+
+
+@dataclass(frozen=True)
+class QuantTree:
+    """The ragged batch of draft trees that attends to a QuantCache; mirrors the C struct sb_quant_tree."""
+    n_q_heads: int
+    prefix_len: torch.Tensor     # int32 [B]
+    node_offsets: torch.Tensor   # int32 [B+1]
+    parent: torch.Tensor         # int32 [total_nodes]
+    max_nodes: int
+    max_prefix: int
+
+    def __post_init__(self):
+        s = _QuantTree()
+        dev = self.prefix_len.device
+        s.n_q_heads, s.total_nodes = self.n_q_heads, self.parent.numel()
+        s.max_nodes, s.max_prefix = self.max_nodes, self.max_prefix
+        s.prefix_len = _addr(self.prefix_len, torch.int32, dev)
+        s.node_offsets = _addr(self.node_offsets, torch.int32, dev, self.prefix_len.numel() + 1)
+        s.parent = _addr(self.parent, torch.int32, dev)
+        object.__setattr__(self, "c_struct", s)
+        object.__setattr__(self, "c_ref", C.addressof(s))
+
+
+def _rows_of(t, heads, dim, device, what):
+    """(address, elements between rows) of bf16 rows [..., heads, dim] whose rows are contiguous inside: a whole tensor or
+    a slice of a fused projection."""
+    if t.dtype != torch.bfloat16:
+        raise TypeError(f"{what}: expected torch.bfloat16, got {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{what}: expected a tensor on {device}, got {t.device}")
+    shape, stride = t.shape, t.stride()
+    if shape[-2] != heads or shape[-1] != dim or stride[-1] != 1 or (heads > 1 and stride[-2] != dim):
+        raise ValueError(f"{what}: expected rows of [{heads}, {dim}] that are contiguous inside, got {tuple(shape)} with strides {stride}")
+    return t.data_ptr(), (stride[-3] if shape[-3] > 1 else heads * dim)
+
+
+def sb_tree_attention_quant_workspace_bytes(kv: QuantCache, tree: QuantTree, total_q: int, *, num_splits: int = 0,
+                                            window: int = 0, sinks: int = 0) -> int:
+    return int(load().sb_tree_attention_quant_workspace_bytes(kv.c_ref, tree.c_ref, total_q, window, sinks, num_splits))
+
+
+def sb_tree_attention_quant(kv: QuantCache, tree: QuantTree, q, k_nodes, v_nodes, *, layer=0, window=0, sinks=0, out=None,
+                            lse=None, q_node_begin=None, q_offsets=None, scale=0.0, num_splits=0, workspace=None,
+                            status=None, want_lse=True):
+    """q bf16 [total_q, Hq, D], k_nodes / v_nodes bf16 [total_nodes, Hkv, D] (rows may be strided) over the 8-bit prefix ->
+    (out bf16 [total_q, Hq, D], lse fp32 [total_q, Hq] or None, status [B]).  window > 0: a node at position x sees
+    positions above x - window and the first `sinks`."""
+    dev = _cuda_device(q)
+    total_q = q.shape[0]
+    Hq, D, B = tree.n_q_heads, kv.head_dim, kv.batch
+    if tree.prefix_len.numel() != B:
+        raise ValueError("the tree batch and the cache have different numbers of sequences")
+    if kv.k_codes.device != dev or tree.parent.device != dev:
+        raise ValueError(f"cache, tree and q must all be on {dev}")
+    q_ptr, q_stride = _rows_of(q, Hq, D, dev, "q")
+    total = tree.parent.numel()
+    if k_nodes.shape[0] != total or v_nodes.shape[0] != total:
+        raise ValueError(f"k_nodes and v_nodes must have {total} rows")
+    k_ptr, k_stride = _rows_of(k_nodes, kv.n_kv_heads, D, dev, "k_nodes")
+    v_ptr, v_stride = _rows_of(v_nodes, kv.n_kv_heads, D, dev, "v_nodes")
+    if k_stride != v_stride:
+        raise ValueError("k_nodes and v_nodes must have the same stride between rows")
+    if q_node_begin is None and q_offsets is None and total_q != total:
+        raise ValueError(f"q must have one row for each of the {total} nodes, or q_offsets must say where its rows are")
+    out = torch.empty((total_q, Hq, D), dtype=torch.bfloat16, device=dev) if out is None else out
+    if lse is None and want_lse:
+        lse = torch.empty((total_q, Hq), dtype=torch.float32, device=dev)
+    status = torch.empty(B, dtype=torch.int32, device=dev) if status is None else status
+    lib = load()
+    if workspace is None:
+        need = lib.sb_tree_attention_quant_workspace_bytes(kv.c_ref, tree.c_ref, total_q, window, sinks, num_splits)
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+    rc = lib.sb_tree_attention_quant(
+        kv.c_ref, layer, tree.c_ref, k_ptr, v_ptr, k_stride, _addr(q_node_begin, torch.int32, dev, B),
+        _addr(q_offsets, torch.int32, dev, B), total_q, q_ptr, q_stride, _addr(out, torch.bfloat16, dev, total_q * Hq * D),
+        _addr(lse, torch.float32, dev, total_q * Hq), scale, window, sinks, num_splits, _addr(workspace, torch.uint8, dev),
+        workspace.numel(), _addr(status, torch.int32, dev, B), _stream_of(dev))
+    _check(rc, "sb_tree_attention_quant")
+    return out, lse, status
+
+
+def sb_kv_append_quant(kv: QuantCache, k_rows, v_rows, row_offsets, length, *, max_rows, path_nodes=None, accept_len=None,
+                       max_depth=0, new_len=None, status=None):
+    """Appends bf16 rows k_rows / v_rows [(layers,) rows, Hkv, D] to the cache behind length int32 [B]: rows
+    row_offsets[b] .. row_offsets[b+1] - 1, or with path_nodes and accept_len (as sb_verify_accept leaves them) the accepted
+    path's rows.  max_rows bounds the rows of a sequence.  -> (new_len [B], status [B])."""
+    dev = _cuda_device(k_rows)
+    if kv.k_codes.device != dev:
+        raise ValueError(f"cache and rows must both be on {dev}")
+    B = kv.batch
+    if k_rows.shape != v_rows.shape or k_rows.stride() != v_rows.stride():
+        raise ValueError("k_rows and v_rows must have the same shape and strides")
+    if k_rows.dim() == 4:
+        if k_rows.shape[0] != kv.n_layers:
+            raise ValueError(f"the rows' first dimension must be the cache's {kv.n_layers} layers")
+        layer_stride = k_rows.stride(0) if kv.n_layers > 1 else 0
+    elif k_rows.dim() == 3 and kv.n_layers == 1:
+        layer_stride = 0
+    else:
+        raise ValueError("rows must be [layers, rows, n_kv_heads, head_dim]")
+    k_ptr, stride = _rows_of(k_rows, kv.n_kv_heads, kv.head_dim, dev, "k_rows")
+    v_ptr, _ = _rows_of(v_rows, kv.n_kv_heads, kv.head_dim, dev, "v_rows")
+    new_len = torch.empty(B, dtype=torch.int32, device=dev) if new_len is None else new_len
+    status = torch.empty(B, dtype=torch.int32, device=dev) if status is None else status
+    rc = load().sb_kv_append_quant(
+        kv.c_ref, k_ptr, v_ptr, stride, layer_stride, _addr(row_offsets, torch.int32, dev, B + 1), k_rows.shape[-3],
+        _addr(path_nodes, torch.int32, dev, B * (max_depth + 1)), _addr(accept_len, torch.int32, dev, B), max_depth, max_rows,
+        _addr(length, torch.int32, dev, B), _addr(new_len, torch.int32, dev, B), _addr(status, torch.int32, dev, B),
+        _stream_of(dev))
+    _check(rc, "sb_kv_append_quant")
+    return new_len, status
+
+
+# ---- pages of a cache ------------------------------------------------------------------------------------------------
+
+@dataclass(frozen=True)
+class PagePool:
+    """Bookkeeping of a paged cache (int32 device tensors); mirrors the C struct sb_page_pool.  page_table [slots,
+    max_pages] (-1 behind a slot's pages), held [slots], refs [num_pages] (0 = free)."""
+    page_size: int
+    page_table: torch.Tensor
+    held: torch.Tensor
+    refs: torch.Tensor
+
+    def __post_init__(self):
+        s = _PagePool()
+        dev = self.page_table.device
+        if self.page_table.dim() != 2:
+            raise ValueError("page_table must be [slots, max_pages]")
+        s.page_size, s.num_pages = self.page_size, self.refs.numel()
+        s.n_slots, s.max_pages = self.page_table.shape
+        s.page_table = _addr(self.page_table, torch.int32, dev)
+        s.held = _addr(self.held, torch.int32, dev, s.n_slots)
+        s.refs = _addr(self.refs, torch.int32, dev)
+        object.__setattr__(self, "c_struct", s)
+        object.__setattr__(self, "c_ref", C.addressof(s))
+
+    @classmethod
+    def empty(cls, n_slots, max_pages, num_pages, page_size, device="cuda"):
+        """A pool of free pages."""
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(page_size, torch.full((n_slots, max_pages), -1, **i32), torch.zeros(n_slots, **i32), torch.zeros(num_pages, **i32))
+
+
+@dataclass(frozen=True)
+class PageCopies:
+    """The (source, destination) page pairs that sb_pages_reserve / sb_pages_compact leave for sb_pages_copy: src, dst
+    int32 [room], -1 behind the count[0] pairs."""
+    src: torch.Tensor
+    dst: torch.Tensor
+    count: torch.Tensor
+
+    @classmethod
+    def empty(cls, room, device="cuda"):
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(torch.full((room,), -1, **i32), torch.full((room,), -1, **i32), torch.zeros(1, **i32))
+
+
+@dataclass(frozen=True)
+class PageArrays:
+    """The arrays that a page id indexes, each [pages, ...] or [layers, pages, ...], contiguous: K and V codes and scales of
+    an 8-bit cache, or K and V of a bf16 one."""
+    tensors: list
+    n_layers: int
+    num_pages: int
+
+    def __post_init__(self):
+        arr = (_PageArray * len(self.tensors))()
+        for a, t in zip(arr, self.tensors):
+            lead = t.shape[:2] if self.n_layers > 1 or t.shape[0] != self.num_pages else (1, t.shape[0])
+            if tuple(lead) != (self.n_layers, self.num_pages):
+                raise ValueError(f"expected [{self.n_layers}, {self.num_pages}, ...] (or without layers), got {tuple(t.shape)}")
+            layer = t.numel() // self.n_layers * t.element_size()
+            a.base, a.page_bytes, a.layer_stride = _addr(t, t.dtype, self.tensors[0].device), layer // self.num_pages, layer
+        object.__setattr__(self, "c_array", arr)
+        object.__setattr__(self, "c_ref", C.addressof(arr))
+
+
+def sb_pages_workspace_bytes(pool: PagePool, n: int) -> int:
+    return int(load().sb_pages_workspace_bytes(pool.c_ref, n))
+
+
+def _pages_call(pool, n, workspace, status, entries):
+    dev = _cuda_device(pool.page_table)
+    if workspace is None:
+        workspace = torch.empty(max(sb_pages_workspace_bytes(pool, n), 256), dtype=torch.uint8, device=dev)
+    status = torch.empty(entries, dtype=torch.int32, device=dev) if status is None else status
+    return dev, (_addr(workspace, torch.uint8, dev), workspace.numel(), _addr(status, torch.int32, dev, entries), _stream_of(dev)), status, workspace
+
+
+def sb_pages_fork(pool: PagePool, src, dst, length, *, workspace=None, status=None):
+    """Slots dst (int32 [n], empty) share the pages of slots src that hold their first `length` positions.  -> status [n]."""
+    n = src.numel()
+    dev, tail, status, workspace = _pages_call(pool, n, workspace, status, n)
+    rc = load().sb_pages_fork(pool.c_ref, n, _addr(src, torch.int32, dev), _addr(dst, torch.int32, dev, n),
+                              _addr(length, torch.int32, dev, n), *tail)
+    _check(rc, "sb_pages_fork")
+    return status
+
+
+def sb_pages_reserve(pool: PagePool, slots, keep_len, new_len, copies: PageCopies, *, workspace=None, status=None):
+    """Makes positions [keep_len, new_len) of the slots writable: adds pages, and replaces shared ones; what has to be copied
+    goes to `copies` (room for n pairs).  -> status [n]."""
+    n = slots.numel()
+    dev, tail, status, workspace = _pages_call(pool, n, workspace, status, n)
+    if copies.src.numel() < n:
+        raise ValueError(f"copies needs room for {n} pairs")
+    rc = load().sb_pages_reserve(pool.c_ref, n, _addr(slots, torch.int32, dev), _addr(keep_len, torch.int32, dev, n),
+                                 _addr(new_len, torch.int32, dev, n), _addr(copies.src, torch.int32, dev),
+                                 _addr(copies.dst, torch.int32, dev, copies.src.numel()), _addr(copies.count, torch.int32, dev, 1), *tail)
+    _check(rc, "sb_pages_reserve")
+    return status
+
+
+def sb_pages_release(pool: PagePool, slots, keep_len, *, workspace=None, status=None):
+    """The slots keep the pages of their first keep_len positions.  -> status [n]."""
+    n = slots.numel()
+    dev, tail, status, workspace = _pages_call(pool, n, workspace, status, n)
+    rc = load().sb_pages_release(pool.c_ref, n, _addr(slots, torch.int32, dev), _addr(keep_len, torch.int32, dev, n), *tail)
+    _check(rc, "sb_pages_release")
+    return status
+
+
+def sb_pages_compact(pool: PagePool, copies: PageCopies, *, n_used=None, workspace=None, status=None):
+    """Moves the pages in use to the front of the pool; `copies` (room for num_pages // 2 pairs) says what sb_pages_copy
+    has to move.  -> status [1]."""
+    dev, tail, status, workspace = _pages_call(pool, 0, workspace, status, 1)
+    rc = load().sb_pages_compact(pool.c_ref, _addr(copies.src, torch.int32, dev), _addr(copies.dst, torch.int32, dev, copies.src.numel()),
+                                 copies.src.numel(), _addr(copies.count, torch.int32, dev, 1), _addr(n_used, torch.int32, dev, 1), *tail)
+    _check(rc, "sb_pages_compact")
+    return status
+
+
+def sb_pages_copy(arrays: PageArrays, copies: PageCopies):
+    """Copies the contents of the pages in `copies`, every layer of every array, in one launch."""
+    dev = _cuda_device(copies.src)
+    if arrays.tensors[0].device != dev:
+        raise ValueError(f"expected arrays on {dev}")
+    rc = load().sb_pages_copy(arrays.c_ref, len(arrays.tensors), arrays.n_layers, arrays.num_pages, _addr(copies.src, torch.int32, dev),
+                              _addr(copies.dst, torch.int32, dev, copies.src.numel()), _addr(copies.count, torch.int32, dev, 1),
+                              copies.src.numel(), _stream_of(dev))
+    _check(rc, "sb_pages_copy")
 
 
 # ---- hooks of the test and checked builds (include/specblock_test.h); use inside build_variant(...) ----

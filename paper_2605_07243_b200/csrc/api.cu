@@ -51,6 +51,7 @@ extern "C" const char* sb_status_string(sb_status s) {
     case SB_ERR_INVALID_TREE: return "invalid tree";
     case SB_ERR_BOUNDS: return "position or page outside the cache";
     case SB_ERR_CUDA: return "CUDA call failed";
+    case SB_ERR_NO_PAGES: return "too few free pages";
   }
   return "unknown status";
 }

@@ -1,0 +1,185 @@
+// sb_tree_attention_quant: argument checks, choice of kernel and of KV chunks, and the merge of chunks that do not share
+// a cluster.
+#include "quant_attention.cuh"
+
+namespace sb {
+
+// One warp per row: log-sum-exp merge of the clusters' partials.  A NaN partial makes the row NaN.
+template <int D>
+__global__ void __launch_bounds__(256) quant_merge_kernel(const QuantAttnParams p) {
+  constexpr int EPL = D / 32;
+  pdl_wait();
+  pdl_release();
+  const int b = blockIdx.y;
+  const QuantSeq si = load_quant_seq(p, b);
+  if (!si.can_write) return;
+  const int Hq = p.tree.n_q_heads, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rr = blockIdx.x * 8 + warp;
+  if (rr >= si.nq * Hq) return;
+  const long long rows_all = (long long)p.total_q * Hq;
+  const long long grow = (long long)si.q_off * Hq + rr;
+  if (!SB_CHECKED_ACCESS(grow, rows_all, &p.status[b])) return;
+  float M = -INFINITY;
+  for (int s = 0; s < p.outer; ++s) M = fmaxf(M, p.part_lse[s * rows_all + grow]);
+  float acc[EPL], sum = 0.f;
+#pragma unroll
+  for (int e = 0; e < EPL; ++e) acc[e] = 0.f;
+#pragma unroll 4
+  for (int s = 0; s < p.outer; ++s) {
+    const float lse2 = p.part_lse[s * rows_all + grow];
+    const float w = lse2 == -INFINITY ? 0.f : fast_exp2(lse2 - M);
+    const float* src = p.part_o + (s * rows_all + grow) * D + lane * EPL;
+    sum += w;
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) acc[e] = fmaf(w, src[e], acc[e]);
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + grow * D + lane * EPL);
+#pragma unroll
+  for (int e = 0; e < EPL; e += 2) dst[e / 2] = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
+  if (p.lse && lane == 0) p.lse[grow] = sum == 0.f ? 0.f : (M + log2f(sum)) * kLn2;
+}
+
+static int quant_num_sms() {
+  static PerDeviceInt cache;
+  return cache.get([]() {
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) {
+      cudaGetLastError();
+      sms = 148;
+    }
+    return sms;
+  }, 148);
+}
+
+struct QuantPlan {
+  int cluster, outer, row_tiles;
+};
+
+// Chunks per (sequence, KV head, 16-row tile): enough for two CTAs on every SM, grouped into clusters of up to 8.
+static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree, int total_q, int window, int sinks, int num_splits) {
+  QuantPlan pl;
+  const int G = tree->n_q_heads / kv->n_kv_heads;
+  const int nq = tree->max_nodes < total_q ? tree->max_nodes : total_q;
+  pl.row_tiles = ceil_div((nq > 0 ? nq : 1) * G, 16);
+  long long keys = tree->max_prefix;
+  if (window > 0 && (long long)window + sinks + 64 < keys) keys = (long long)window + sinks + 64;
+  const int groups = (int)((keys + 31) / 32) + ceil_div(tree->max_nodes, 32);
+  const long long units = (long long)kv->batch * kv->n_kv_heads * pl.row_tiles;
+  int s;
+  if (num_splits > 0) {
+    s = num_splits;
+  } else {
+    s = (int)(2LL * quant_num_sms() / units);
+    const int most = ceil_div(groups, 4);  // a group for each of the four warps
+    if (s > most) s = most;
+    if (s > 64) s = 64;
+  }
+  if (s > groups) s = groups;
+  if (s < 1) s = 1;
+  if (s > kQuantMaxCluster && num_splits == 0) s = s / kQuantMaxCluster * kQuantMaxCluster;
+  pl.cluster = 1;
+  for (int c = kQuantMaxCluster; c >= 1; --c)
+    if (s % c == 0) { pl.cluster = c; break; }
+  pl.outer = s / pl.cluster;
+  return pl;
+}
+
+static sb_status check_quant_call(const sb_quant_cache* kv, const sb_quant_tree* tree, int window, int sinks, int num_splits) {
+  const sb_status st = check_quant_cache(kv);
+  if (st != SB_OK) return st;
+  if (!tree || !tree->prefix_len || !tree->node_offsets || !tree->parent || tree->n_q_heads < 1 ||
+      tree->n_q_heads % kv->n_kv_heads != 0 || tree->total_nodes < 0 || tree->max_prefix < 0)
+    return SB_ERR_INVALID_ARG;
+  if (window < 0 || sinks < 0 || (window == 0 && sinks != 0) || num_splits < 0) return SB_ERR_INVALID_ARG;
+  if (tree->n_q_heads / kv->n_kv_heads > 16) return SB_ERR_UNSUPPORTED;
+  if (tree->max_nodes < 1 || tree->max_nodes > SB_MAX_NODES) return SB_ERR_UNSUPPORTED;
+  if (kv->batch > 65535 || tree->max_prefix > 0x7fffffff - 256 || window > 0x7fffffff - 256) return SB_ERR_UNSUPPORTED;
+  return SB_OK;
+}
+
+static size_t quant_workspace_bytes(const sb_quant_cache* kv, const sb_quant_tree* tree, int total_q, int outer) {
+  if (outer <= 1) return 0;
+  const size_t rows = (size_t)total_q * tree->n_q_heads;
+  const size_t o = (size_t)outer * rows * kv->head_dim * sizeof(float), l = (size_t)outer * rows * sizeof(float);
+  return ((o + 255) & ~(size_t)255) + ((l + 255) & ~(size_t)255);
+}
+
+}  // namespace sb
+
+extern "C" size_t sb_tree_attention_quant_workspace_bytes(const sb_quant_cache* kv, const sb_quant_tree* tree,
+                                                          int32_t total_q, int32_t window, int32_t sinks,
+                                                          int32_t num_splits) {
+  if (sb::check_quant_call(kv, tree, window, sinks, num_splits) != SB_OK || total_q < 0) return 0;
+  return sb::quant_workspace_bytes(kv, tree, total_q, sb::plan_quant(kv, tree, total_q, window, sinks, num_splits).outer);
+}
+
+extern "C" sb_status sb_tree_attention_quant(const sb_quant_cache* kv, int32_t layer, const sb_quant_tree* tree,
+                                             const void* k_nodes, const void* v_nodes, int64_t node_stride,
+                                             const int32_t* q_node_begin, const int32_t* q_offsets, int32_t total_q,
+                                             const void* q, int64_t q_stride, void* out, float* lse, float scale,
+                                             int32_t window, int32_t sinks, int32_t num_splits, void* workspace,
+                                             size_t workspace_bytes, int32_t* status, void* stream) {
+  sb::TraceRange trace_range("sb_tree_attention_quant");
+  using namespace sb;
+  const sb_status st = check_quant_call(kv, tree, window, sinks, num_splits);
+  if (st != SB_OK) return st;
+  if (!k_nodes || !v_nodes || !q || !out || !status || total_q < 1 || !(scale >= 0.f) || layer < 0 || layer >= kv->n_layers)
+    return SB_ERR_INVALID_ARG;
+  if (q_node_begin && !q_offsets) return SB_ERR_INVALID_ARG;
+  const int D = kv->head_dim;
+  const int64_t node_width = (int64_t)kv->n_kv_heads * D, q_width = (int64_t)tree->n_q_heads * D;
+  if (node_stride == 0) node_stride = node_width;
+  if (q_stride == 0) q_stride = q_width;
+  if (node_stride < node_width || node_stride % 8 != 0 || q_stride < q_width || q_stride % 8 != 0) return SB_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out) | reinterpret_cast<uintptr_t>(k_nodes) |
+       reinterpret_cast<uintptr_t>(v_nodes)) & 15)
+    return SB_ERR_INVALID_ARG;
+  QuantAttnParams p;
+  p.kv = *kv;
+  p.k_codes = static_cast<const uint8_t*>(kv->k_codes) + layer * kv->codes_layer_stride;
+  p.v_codes = static_cast<const uint8_t*>(kv->v_codes) + layer * kv->codes_layer_stride;
+  p.k_scale = kv->k_scale + layer * kv->scale_layer_stride;
+  p.v_scale = kv->v_scale + layer * kv->scale_layer_stride;
+  p.tree = *tree;
+  p.k_nodes = static_cast<const bf16*>(k_nodes);
+  p.v_nodes = static_cast<const bf16*>(v_nodes);
+  p.node_stride = node_stride;
+  p.q_node_begin = q_node_begin;
+  p.q_offsets = q_offsets;
+  p.total_q = total_q;
+  p.q = static_cast<const bf16*>(q);
+  p.q_stride = q_stride;
+  p.out = static_cast<bf16*>(out);
+  p.lse = lse;
+  p.scale_log2 = (scale > 0.f ? scale : 1.0f / sqrtf((float)D)) * 1.4426950408889634f;
+  p.window = window;
+  p.sinks = sinks;
+  p.status = status;
+  p.G = tree->n_q_heads / kv->n_kv_heads;
+  p.part_o = nullptr;
+  p.part_lse = nullptr;
+  const QuantPlan pl = plan_quant(kv, tree, total_q, window, sinks, num_splits);
+  p.num_splits = pl.cluster * pl.outer;
+  p.outer = pl.outer;
+  if (pl.outer > 1) {
+    if (!workspace || workspace_bytes < quant_workspace_bytes(kv, tree, total_q, pl.outer) ||
+        (reinterpret_cast<uintptr_t>(workspace) & 255))
+      return SB_ERR_WORKSPACE;
+    const size_t rows = (size_t)total_q * tree->n_q_heads;
+    p.part_o = static_cast<float*>(workspace);
+    p.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) +
+                                          (((size_t)pl.outer * rows * D * sizeof(float) + 255) & ~(size_t)255));
+  }
+  const dim3 grid(p.num_splits, pl.row_tiles * kv->n_kv_heads, kv->batch);
+  if (grid.y > 65535) return SB_ERR_UNSUPPORTED;
+  p.sort_seqs = kv->batch > 1 && kv->batch <= SB_MAX_NODES &&
+                (long long)grid.x * grid.y * grid.z > 2LL * quant_num_sms() ? 1 : 0;
+  cudaStream_t cs = static_cast<cudaStream_t>(stream);
+  const sb_status ls = launch_quant_rows(p, grid, pl.cluster, cs);
+  if (ls != SB_OK || pl.outer == 1) return ls;
+  const dim3 mgrid(ceil_div(tree->max_nodes * tree->n_q_heads, 8), kv->batch);
+  return D == 64 ? launch_dependent(quant_merge_kernel<64>, mgrid, dim3(256), cs, p)
+                 : launch_dependent(quant_merge_kernel<128>, mgrid, dim3(256), cs, p);
+}
