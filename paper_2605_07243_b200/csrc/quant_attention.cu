@@ -54,24 +54,52 @@ static int quant_num_sms() {
 }
 
 struct QuantPlan {
-  int cluster, outer, row_tiles;
+  bool tc;                         // the tcgen05 kernel; else the 16-row kernel
+  int cluster, outer, grid_tiles;  // grid_tiles: row tiles (16 rows) or pairs of row tiles (2 x 128 rows) per KV head
 };
 
-// Chunks per (sequence, KV head, 16-row tile): enough for two CTAs on every SM, grouped into clusters of up to 8.
 static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree, int total_q, int window, int sinks, int num_splits) {
   QuantPlan pl;
   const int G = tree->n_q_heads / kv->n_kv_heads;
   const int nq = tree->max_nodes < total_q ? tree->max_nodes : total_q;
-  pl.row_tiles = ceil_div((nq > 0 ? nq : 1) * G, 16);
-  long long keys = tree->max_prefix;
+  const int rows = (nq > 0 ? nq : 1) * G;
+  long long keys = tree->max_prefix;  // visible ones, at most
   if (window > 0 && (long long)window + sinks + 64 < keys) keys = (long long)window + sinks + 64;
-  const int groups = (int)((keys + 31) / 32) + ceil_div(tree->max_nodes, 32);
-  const long long units = (long long)kv->batch * kv->n_kv_heads * pl.row_tiles;
+  const int sms = quant_num_sms();
+  pl.tc = rows > 16;
+  pl.cluster = 1;
+  if (pl.tc) {
+    // CTAs run in waves of one per SM.  A CTA costs its key blocks (both streams work on every block when there are two
+    // row tiles, else on every second one) plus a fixed start and end; every chunk beyond the first writes
+    // and re-reads fp32 partials of all rows.
+    pl.grid_tiles = ceil_div(rows, 256);
+    const int blocks = (int)((keys + 127) / 128) + (window > 0 ? 2 : 0) + 1;
+    const long long units = (long long)kv->batch * kv->n_kv_heads * pl.grid_tiles;
+    const double per_block = rows > 128 ? 1.4 : 0.7, fixed = 6.0;
+    const double partial = 2.0 * (double)total_q * tree->n_q_heads * kv->head_dim * 4.0 / 5e6;
+    int best = 1;
+    double best_cost = 0.0;
+    const int most = num_splits > 0 ? 1 : (blocks < 64 ? blocks : 64);
+    for (int s = 1; s <= most; ++s) {
+      const long long waves = (units * s + sms - 1) / sms;
+      const double cost = (double)waves * (ceil_div(blocks, s) * per_block + fixed) + (s > 1 ? partial * s + 3.0 : 0.0);
+      if (s == 1 || cost < best_cost) {
+        best = s;
+        best_cost = cost;
+      }
+    }
+    pl.outer = num_splits > 0 ? (num_splits < blocks ? num_splits : blocks) : best;
+    return pl;
+  }
+  // Chunks per (sequence, KV head): enough for two CTAs on every SM, grouped into clusters of up to 8.
+  pl.grid_tiles = ceil_div(rows, 16);
+  const int groups = (int)((keys + 31) / 32) + (window > 0 ? 2 : 0) + ceil_div(tree->max_nodes, 32);
+  const long long units = (long long)kv->batch * kv->n_kv_heads * pl.grid_tiles;
   int s;
   if (num_splits > 0) {
     s = num_splits;
   } else {
-    s = (int)(2LL * quant_num_sms() / units);
+    s = (int)(2LL * sms / units);
     const int most = ceil_div(groups, 4);  // a group for each of the four warps
     if (s > most) s = most;
     if (s > 64) s = 64;
@@ -79,7 +107,6 @@ static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree,
   if (s > groups) s = groups;
   if (s < 1) s = 1;
   if (s > kQuantMaxCluster && num_splits == 0) s = s / kQuantMaxCluster * kQuantMaxCluster;
-  pl.cluster = 1;
   for (int c = kQuantMaxCluster; c >= 1; --c)
     if (s % c == 0) { pl.cluster = c; break; }
   pl.outer = s / pl.cluster;
@@ -172,12 +199,12 @@ extern "C" sb_status sb_tree_attention_quant(const sb_quant_cache* kv, int32_t l
     p.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) +
                                           (((size_t)pl.outer * rows * D * sizeof(float) + 255) & ~(size_t)255));
   }
-  const dim3 grid(p.num_splits, pl.row_tiles * kv->n_kv_heads, kv->batch);
+  const dim3 grid(p.num_splits, pl.grid_tiles * kv->n_kv_heads, kv->batch);
   if (grid.y > 65535) return SB_ERR_UNSUPPORTED;
   p.sort_seqs = kv->batch > 1 && kv->batch <= SB_MAX_NODES &&
-                (long long)grid.x * grid.y * grid.z > 2LL * quant_num_sms() ? 1 : 0;
+                (long long)grid.x * grid.y * grid.z > (pl.tc ? 1LL : 2LL) * quant_num_sms() ? 1 : 0;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  const sb_status ls = launch_quant_rows(p, grid, pl.cluster, cs);
+  const sb_status ls = pl.tc ? launch_quant_tc(p, grid, cs) : launch_quant_rows(p, grid, pl.cluster, cs);
   if (ls != SB_OK || pl.outer == 1) return ls;
   const dim3 mgrid(ceil_div(tree->max_nodes * tree->n_q_heads, 8), kv->batch);
   return D == 64 ? launch_dependent(quant_merge_kernel<64>, mgrid, dim3(256), cs, p)

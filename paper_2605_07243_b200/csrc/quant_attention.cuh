@@ -126,5 +126,6 @@ __device__ inline bool bf16x2_nonfinite(uint32_t w) {
 
 constexpr int kQuantMaxCluster = 8;
 sb_status launch_quant_rows(const QuantAttnParams& p, dim3 grid, int cluster, cudaStream_t cs);
+sb_status launch_quant_tc(const QuantAttnParams& p, dim3 grid, cudaStream_t cs);
 
 }  // namespace sb
