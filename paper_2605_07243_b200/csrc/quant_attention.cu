@@ -4,17 +4,18 @@
 
 namespace sb {
 
-// One warp per row: log-sum-exp merge of the clusters' partials.  A NaN partial makes the row NaN.
-template <int D>
+// Log-sum-exp merge of the chunks' partials, 16 bytes of a row per lane.  PB16: bf16 partials (tcgen05 kernel), else fp32.
+// A NaN partial makes the row NaN.
+template <int D, bool PB16>
 __global__ void __launch_bounds__(256) quant_merge_kernel(const QuantAttnParams p) {
-  constexpr int EPL = D / 32;
+  constexpr int EPL = PB16 ? 8 : 4, LPR = D / EPL, RPW = 32 / LPR;
   pdl_wait();
   pdl_release();
   const int b = blockIdx.y;
   const QuantSeq si = load_quant_seq(p, b);
   if (!si.can_write) return;
   const int Hq = p.tree.n_q_heads, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int rr = blockIdx.x * 8 + warp;
+  const int rr = (blockIdx.x * 8 + warp) * RPW + lane / LPR, col = lane % LPR;
   if (rr >= si.nq * Hq) return;
   const long long rows_all = (long long)p.total_q * Hq;
   const long long grow = (long long)si.q_off * Hq + rr;
@@ -27,17 +28,26 @@ __global__ void __launch_bounds__(256) quant_merge_kernel(const QuantAttnParams 
 #pragma unroll 4
   for (int s = 0; s < p.outer; ++s) {
     const float lse2 = p.part_lse[s * rows_all + grow];
+    const uint4 raw = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p.part_o) +
+                                                      ((s * rows_all + grow) * D + col * EPL) * (PB16 ? 2 : 4));
     const float w = lse2 == -INFINITY ? 0.f : fast_exp2(lse2 - M);
-    const float* src = p.part_o + (s * rows_all + grow) * D + lane * EPL;
     sum += w;
+    const uint32_t u[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) acc[e] = fmaf(w, src[e], acc[e]);
+    for (int e = 0; e < 4; ++e) {
+      if (PB16) {
+        acc[(2 * e) % EPL] = fmaf(w, __uint_as_float(u[e] << 16), acc[(2 * e) % EPL]);
+        acc[(2 * e + 1) % EPL] = fmaf(w, __uint_as_float(u[e] & 0xFFFF0000u), acc[(2 * e + 1) % EPL]);
+      } else {
+        acc[e] = fmaf(w, __uint_as_float(u[e]), acc[e]);
+      }
+    }
   }
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + grow * D + lane * EPL);
+  uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + grow * D + col * EPL);
 #pragma unroll
   for (int e = 0; e < EPL; e += 2) dst[e / 2] = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
-  if (p.lse && lane == 0) p.lse[grow] = sum == 0.f ? 0.f : (M + log2f(sum)) * kLn2;
+  if (p.lse && col == 0) p.lse[grow] = sum == 0.f ? 0.f : (M + log2f(sum)) * kLn2;
 }
 
 static int quant_num_sms() {
@@ -184,6 +194,8 @@ extern "C" sb_status sb_tree_attention_quant(const sb_quant_cache* kv, int32_t l
   p.window = window;
   p.sinks = sinks;
   p.status = status;
+  p.block_shift = 0;
+  while ((1 << p.block_shift) < kv->scale_block) ++p.block_shift;
   p.G = tree->n_q_heads / kv->n_kv_heads;
   p.part_o = nullptr;
   p.part_lse = nullptr;
@@ -206,7 +218,10 @@ extern "C" sb_status sb_tree_attention_quant(const sb_quant_cache* kv, int32_t l
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
   const sb_status ls = pl.tc ? launch_quant_tc(p, grid, cs) : launch_quant_rows(p, grid, pl.cluster, cs);
   if (ls != SB_OK || pl.outer == 1) return ls;
-  const dim3 mgrid(ceil_div(tree->max_nodes * tree->n_q_heads, 8), kv->batch);
-  return D == 64 ? launch_dependent(quant_merge_kernel<64>, mgrid, dim3(256), cs, p)
-                 : launch_dependent(quant_merge_kernel<128>, mgrid, dim3(256), cs, p);
+  const int rows_max = tree->max_nodes * tree->n_q_heads;
+  auto merge = [&](auto kernel, int rows_per_cta) {
+    return launch_dependent(kernel, dim3(ceil_div(rows_max, rows_per_cta), kv->batch), dim3(256), cs, p);
+  };
+  if (pl.tc) return D == 64 ? merge(quant_merge_kernel<64, true>, 8 * 4) : merge(quant_merge_kernel<128, true>, 8 * 2);
+  return D == 64 ? merge(quant_merge_kernel<64, false>, 8 * 2) : merge(quant_merge_kernel<128, false>, 8);
 }

@@ -32,6 +32,7 @@ struct QuantAttnParams {
   float* part_lse;  // [outer][total_q * Hq]    base-2 log-sum-exp of each
   int* status;
   int G;
+  int block_shift;  // log2 of the tokens per scale block
   int sort_seqs;    // 1: grid index z is the rank of a sequence by length, longest first
 };
 

@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(QR_THREADS, 2) quant_rows_kernel(const QuantAt
       }
       if (lane < 4) {
         const int h = lane & 1;
-        const long long off = half_row[h] / p.kv.scale_block * Hkv + g;
+        const long long off = ((h == 0 ? half_row[0] : half_row[1]) >> p.block_shift) * Hkv + g;
         const float* src = (lane < 2 ? p.k_scale : p.v_scale) + off;
         const uint32_t dst = static_cast<uint32_t>(__cvta_generic_to_shared(&s_scale[warp][i % QR_STAGES][lane]));
         asm volatile("cp.async.ca.shared.global [%0], [%1], 4;\n" ::"r"(dst), "l"(src));

@@ -1,47 +1,54 @@
 // Tree attention over an 8-bit prefix on the tensor cores (tcgen05 + TMEM, sm_100a), for tiles of 128 packed rows.
 //
-// tcgen05 takes operands of one width only, and Q and P would lose what bf16 outputs need as e4m3.  So the codes become
-// fp16 on their way into shared memory (exact: every e4m3 value is an fp16 value): four converter warps load 16
-// codes per thread from global memory, convert them in registers and store them in the operand layout.  The
-// next block's codes wait in registers meanwhile, so global latency hides behind the conversion of the present one,
-// and shared memory holds fp16 tiles only (two of K, two of V).
+// S = Q K^T runs on the codes as they are (kind::f8f6f4, K straight from a TMA tile in shared memory): a bf16 number scaled by its
+// row's power of two is the sum of two e4m3 numbers (eight significant bits are four and a signed four; elements 2^-10
+// and more below the row's largest lose what is below 2^-18 of it), so Q is held as two e4m3 terms and S costs two
+// products at twice the 16-bit rate.  P would need a range that two e4m3 terms do not have (a sink with most of the weight
+// beside thousands of small ones), so O = P V runs in fp16: two converter warps turn the V codes into an fp16 tile (exact:
+// every e4m3 value is an fp16 value).  Converting K as well, and loading both through the converters' registers, took longer
+// than everything else in the kernel: 3000 instructions a block in warps that issue one every eight clocks.
 // Scales never touch an element of the stream: a K scale multiplies the scores of its 16 or more columns, a V scale enters the
 // exponent (P' = 2^(s + log2 v - reference), denominator sum P' / v), which the fused multiply-add that forms
-// the exponent does for nothing.  Q is scaled per row by a power of two into fp16's range.
+// the exponent does for nothing.
 //
-// A CTA owns one KV head's chunk of the key list and two "streams" t = 0, 1, each with its own score buffer and
-// accumulator in tensor memory (2 x 128 + 2 x D columns) and its own softmax warpgroup with one thread per row:
-//   two row tiles (mode A): stream t is tile t, every key block is used twice;
-//   one row tile (mode B): stream t takes every second key block; the two accumulators are merged at the end.
-// The first thread of a stream's warpgroup issues its MMAs, O += P_n V then S_{n+1} = Q K^T, when the warpgroup has
-// written P_n: it has nothing else to do until S_{n+1} is there, and the tensor pipe works for one stream while
-// the other stream's threads compute exponentials.  MMAs of one thread complete in order, so a completed S_{n+1} also means
-// that P_n has been read and the accumulator holds it.  (No warp of its own for the issue: 12 warps leave
-// 168 registers a thread, 13 would leave 128, and the scores would spill.)
+// A CTA owns one KV head's chunk of the key list and two "streams" t = 0, 1, each with its own accumulator and two score
+// buffers of 64 keys in tensor memory (2 x D + 4 x 64 columns) and its own softmax warpgroup with one thread per row:
+//   two row tiles (mode A): stream t is tile t and takes both 64-key halves of every key block in turn;
+//   one row tile (mode B): stream t takes half t of every key block; the two accumulators are merged at the end.
+// The MMA warp issues, for step i of each stream in turn, O_t += P_i V and then S_{i+2} = Q K^T into the buffer that P_i was
+// read from.  So a softmax warp always has the next 64 scores waiting while the tensor pipe is busy with the buffer it
+// has just left: with one 128-key buffer per stream the warps spent half of their time waiting for PV and S of their
+// own stream (6400 clocks per key block and pair of tiles against 2100 of tensor work).
 //
-// The softmax thread walks its row's 128 scores in quarters of 32 columns, the next quarter's load in flight.  The
-// reference is raised only when a score exceeds it by 2^8 (P' is fp16: up to 2^15 would do), a rare event that rescales
-// the accumulator and the quarters already written; so the maximum of a whole block is never needed first.
+// The softmax thread does not compute a maximum after its row's first visible key: the reference is raised when the sum of 32
+// probabilities shows that an exponent is far above it (P' is fp16, which ends at 2^16), a rare event that
+// rescales the accumulator.
 //
-// Prefix blocks come from the window's block list (128 keys); the tree's nodes are one last block of their own, whose bf16
-// rows are brought into fp16 by a power of two per 16 rows, as if they were codes.
+// Prefix blocks come from the window's block list (128 keys); the tree's nodes are one last block of their own, scaled by a
+// power of two per 16 rows as if they were codes: K as two e4m3 terms, V as fp16.
 #include "quant_attention.cuh"
 #include "tc_common.cuh"
 
 namespace sb {
 
 constexpr int QT_SOFTMAX = 256;       // warps 0-3: stream 0, warps 4-7: stream 1
-constexpr int QT_CVT_WARP = 8;        // warps 8-11; warp 8 also owns the tensor memory allocation
-constexpr int QT_THREADS = 384;
+constexpr int QT_MMA_WARP = 8;
+constexpr int QT_LOAD_WARP = 9;       // K and V tiles by TMA, scales
+constexpr int QT_CVT_WARP = 10;       // warps 10, 11: V codes -> fp16, and the tree block
+constexpr int QT_THREADS = 384;       // 12 warps leave 168 registers a thread
 constexpr int QT_TMEM_COLS = 512;
 constexpr int QT_SMALL = 8192;
-constexpr float kQuantStep = 8.f;     // the reference follows the maximum in steps of at least 2^8
+constexpr float kQuantLimit = 8192.f; // sum of 32 probabilities relative to the reference beyond which it is raised
 
-enum QtBar { QB_K_FULL0, QB_K_FULL1, QB_K_EMPTY0, QB_K_EMPTY1, QB_V_FULL0, QB_V_FULL1, QB_V_EMPTY0, QB_V_EMPTY1,
-             QB_S_FULL0, QB_S_FULL1, QB_SC0, QB_SC1, QB_SC2, QB_SC3, QB_O_DONE0, QB_O_DONE1, QB_COUNT };
+enum QtBar { QB_P_FULL00, QB_P_FULL01, QB_P_FULL10, QB_P_FULL11,                              // 128 arrivals: a stream's threads
+             QB_V_FULL0, QB_V_FULL1, QB_VR_EMPTY0, QB_VR_EMPTY1,                              // 2: the converter warps
+             QB_K_FULL0, QB_K_FULL1, QB_VR_FULL0, QB_VR_FULL1, QB_SC0, QB_SC1, QB_SC2, QB_SC3, QB_K_EMPTY0, QB_K_EMPTY1,
+             QB_V_EMPTY0, QB_V_EMPTY1, QB_S_FULL00, QB_S_FULL01, QB_S_FULL10, QB_S_FULL11, QB_PV0, QB_PV1, QB_O_DONE,
+             QB_Q_FULL, QB_COUNT };
 
+// Q terms (2 tiles x 2 x 128 D), K codes (2 stages), the tree's second K term, V codes (2 stages), V fp16 (2 stages)
 template <int D>
-constexpr int quant_tc_smem() { return 1024 + QT_SMALL + 6 * TC_BM * D * 2; }
+constexpr int quant_tc_smem() { return 1024 + QT_SMALL + TC_BM * D * (4 + 2 + 1 + 2 + 4); }
 
 __device__ inline uint32_t tc_idesc_f16(int M, int N, int b_mn_major) {
   return (1u << 4) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
@@ -51,6 +58,39 @@ __device__ inline uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+// kind::f8f6f4, e4m3 A and B, both K-major: the same bits with other meanings of the type fields (0 = e4m3)
+__device__ inline uint32_t tc_idesc_e4m3(int M, int N) { return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24); }
+// One lane of the (converged) warp.
+__device__ inline uint32_t elect_one() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}\n" : "=r"(r));
+  return r;
+}
+// The MMA forms of tc_common.cuh for a whole warp of which one lane issues: the operands are the same in every lane, so the
+// compiler keeps them in uniform registers (a lane of its own would move each of them there for every MMA, which
+// costs more issue time than the tensor pipe takes for the MMA).
+__device__ inline void warp_mma_f8(uint32_t elected, uint32_t d_tmem, uint32_t alo, uint32_t blo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 ad, bd;\n\tsetp.ne.b32 p, %5, 0;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "mov.b64 ad, {%1, %3};\n\tmov.b64 bd, {%2, %3};\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], ad, bd, %4, p;\n\t}\n" ::"r"(d_tmem),
+      "r"(alo), "r"(blo), "r"(hi), "r"(idesc), "r"(accumulate), "r"(elected)
+      : "memory");
+}
+__device__ inline void warp_mma_ts(uint32_t elected, uint32_t d_tmem, uint32_t a_tmem, uint32_t blo, uint32_t hi, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t.reg .b64 bd;\n\tsetp.ne.b32 p, %5, 0;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+      "mov.b64 bd, {%2, %3};\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], bd, %4, p;\n\t}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(blo), "r"(hi), "r"(idesc), "r"(accumulate), "r"(elected)
+      : "memory");
+}
+__device__ inline void warp_commit(uint32_t elected, uint64_t* bar) {
+  asm volatile(
+      "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+      "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(smem_u32(bar)), "r"(elected)
+      : "memory");
 }
 // 32 columns without the wait
 __device__ inline void tmem_ld32_async(uint32_t taddr, uint32_t (&r)[32]) {
@@ -74,9 +114,178 @@ __device__ inline void tmem_wait_ld(uint32_t (&r)[32]) {
                : "memory");
 }
 
+// Rescales a row in tensor memory: its accumulator (unless there is none yet) and the quarters of P already written
+// for the present block.  Rare, and out of line: its registers and code stay out of the main loop.
 template <int D>
-__global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttnParams p) {
-  constexpr int TILE = TC_BN * D * 2;   // one fp16 tile of 128 rows
+__device__ __noinline__ void rescale_row(uint32_t o_addr, uint32_t p_addr, int quarters, float factor) {
+  tmem_wait_st();  // what is read back was written by this thread
+  if (o_addr != 0xffffffffu) {
+#pragma unroll 1
+    for (int c = 0; c < D / 16; ++c) {
+      uint32_t r[16];
+      tmem_ld16(o_addr + c * 16, r);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * factor);
+      tmem_st16(o_addr + c * 16, r);
+    }
+  }
+#pragma unroll 1
+  for (int c = 0; c < quarters; ++c) {
+    uint32_t r[16];
+    tmem_ld16(p_addr + 16 * c, r);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r[i]));
+      r[i] = pack_f16(f.x * factor, f.y * factor);
+    }
+    tmem_st16(p_addr + 16 * c, r);
+  }
+  tmem_wait_st();
+}
+
+// log2, exact for powers of two
+__device__ inline float log2_of_scale(float s) {
+  const uint32_t u = __float_as_uint(s);
+  return (float)((int)(u >> 23) - 127) + __log2f(__uint_as_float((u & 0x7FFFFFu) | 0x3F800000u));
+}
+// Byte offset of 16-byte chunk `ch` of row `r` in a tile of D-byte rows, as TMA and the tensor core swizzle them (128-byte rows: XOR with
+// the row's low three bits; 64-byte rows: with bits 1 and 2).
+template <int D>
+__device__ inline uint32_t code_tile_off(int r, int ch) {
+  return (uint32_t)(r * D + ((ch ^ (D == 128 ? (r & 7) : ((r >> 1) & 3))) << 4));
+}
+// Two values -> e4m3 codes of the nearest values and of what is left.
+__device__ inline void split_e4m3(float a, float b, uint16_t& hi, uint16_t& lo) {
+  hi = e4m3x2_of(a, b);
+  const float2 h = float2_of_e4m3x2(hi);
+  lo = e4m3x2_of(a - h.x, b - h.y);
+}
+struct ScaleRing {
+  float *ks, *lsv, *isv;   // [4 slots][8 groups of 16 keys]: K scale, log2 of the V scale, 1 / V scale
+  uint32_t* flag;          // [4 slots]: bits 0-7 the groups with a NaN scale, bits 8-15 those whose V reads as zeros
+};
+
+// Lane -> (row, 16-element chunk) when a warp moves rows of D elements, 32 / (D / 16) rows at a time.  D = 128: eight neighbouring
+// lanes hold four chunks of two rows, not eight of one row: the two fp16 column halves of a row lie in the same banks, two
+// neighbouring rows in different ones.
+template <int D>
+__device__ inline int lane_chunk(int lane) { return D == 128 ? (lane & 3) | ((lane >> 1) & 4) : lane & 3; }
+template <int D>
+__device__ inline int lane_row(int lane) { return D == 128 ? ((lane >> 2) & 1) | ((lane >> 3) & 2) : lane >> 2; }
+
+// 16 node rows (from row 16 * grp of `src`, n of them exist): this lane's 16 elements of each of its rows.  Rows that hold a NaN
+// or an infinity become zeros; their bits are returned.
+template <int D>
+__device__ inline uint32_t node_rows(const bf16* src, long long stride, int n, int grp, int lane, uint4 (&x)[D / 16]) {
+  constexpr int RPI = 512 / D, NI = 16 / RPI;
+  const int ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
+  uint32_t bits = 0;
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const int nd = 16 * grp + i * RPI + r_in;
+    x[2 * i] = x[2 * i + 1] = make_uint4(0, 0, 0, 0);
+    if (nd < n) {
+      const uint4* s4 = reinterpret_cast<const uint4*>(src + nd * stride + ch * 16);
+      x[2 * i] = s4[0];
+      x[2 * i + 1] = s4[1];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    const uint32_t w[8] = {x[2 * i].x, x[2 * i].y, x[2 * i].z, x[2 * i].w, x[2 * i + 1].x, x[2 * i + 1].y, x[2 * i + 1].z, x[2 * i + 1].w};
+    bool nf = false;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) nf |= bf16x2_nonfinite(w[k]);
+    const uint32_t mine = __reduce_or_sync(0xffffffffu, nf ? 1u << r_in : 0u);
+    if ((mine >> r_in) & 1u) x[2 * i] = x[2 * i + 1] = make_uint4(0, 0, 0, 0);
+    bits |= mine << (i * RPI);
+  }
+  return bits;
+}
+// Biased exponent e of the power of two 2^(e - 127) that takes 16 rows to magnitudes below 2^(up + 1).
+template <int N>
+__device__ inline int node_exponent(const uint4 (&x)[N], int up, int least) {
+  uint32_t amax = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) amax = max(amax, max(w[k] & 0x7FFFu, (w[k] >> 16) & 0x7FFFu));
+  }
+  amax = __reduce_max_sync(0xffffffffu, amax);
+  return min(amax < 0x80u ? 127 : max((int)(amax >> 7) - up, least), 253);
+}
+// 16 rows of the tree (group grp).  K side: two e4m3 terms into k1 and k2, the scales of both sides and the bits of bad rows, which the
+// softmax needs.  V side: fp16 into v16.  (Apart, because the V stage may still be read when K is needed.)  Out of line: a
+// few times per CTA.
+template <int D>
+__device__ __noinline__ void node_group(const bf16* k_nodes, const bf16* v_nodes, long long stride, int n, int grp, uint8_t* k1, uint8_t* k2,
+                                        uint8_t* v16, ScaleRing ring, int slot, uint32_t* s_bad) {
+  constexpr int RPI = 512 / D, NI = 16 / RPI;
+  const int lane = threadIdx.x & 31, ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
+  uint4 x[D / 16];
+  uint32_t bits = node_rows<D>(v_nodes, stride, n, grp, lane, x);
+  const int ev = node_exponent(x, 8, 127 - 60);  // (see v_scale_used)
+  float inv = __uint_as_float((uint32_t)(254 - ev) << 23);
+  if (v16) {
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t w[4] = {x[2 * i + k].x, x[2 * i + k].y, x[2 * i + k].z, x[2 * i + k].w};
+        uint32_t h[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) h[c] = pack_f16(__uint_as_float(w[c] << 16) * inv, __uint_as_float(w[c] & 0xFFFF0000u) * inv);
+        *reinterpret_cast<uint4*>(v16 + sw128_chunk_off(16 * grp + i * RPI + r_in, 2 * ch + k, TC_BN)) = make_uint4(h[0], h[1], h[2], h[3]);
+      }
+    return;
+  }
+  bits |= node_rows<D>(k_nodes, stride, n, grp, lane, x);
+  const int ek = node_exponent(x, 7, 1);
+  inv = __uint_as_float((uint32_t)(254 - ek) << 23);
+#pragma unroll
+  for (int i = 0; i < NI; ++i) {
+    uint32_t hi[4], lo[4];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t w[4] = {x[2 * i + k].x, x[2 * i + k].y, x[2 * i + k].z, x[2 * i + k].w};
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint16_t h0, l0, h1, l1;
+        split_e4m3(__uint_as_float(w[2 * c] << 16) * inv, __uint_as_float(w[2 * c] & 0xFFFF0000u) * inv, h0, l0);
+        split_e4m3(__uint_as_float(w[2 * c + 1] << 16) * inv, __uint_as_float(w[2 * c + 1] & 0xFFFF0000u) * inv, h1, l1);
+        hi[2 * k + c] = h0 | ((uint32_t)h1 << 16);
+        lo[2 * k + c] = l0 | ((uint32_t)l1 << 16);
+      }
+    }
+    const uint32_t off = code_tile_off<D>(16 * grp + i * RPI + r_in, ch);
+    *reinterpret_cast<uint4*>(k1 + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    *reinterpret_cast<uint4*>(k2 + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+  }
+  if (lane == 0) {
+    ring.ks[slot * 8 + grp] = __uint_as_float((uint32_t)ek << 23);
+    ring.lsv[slot * 8 + grp] = (float)(ev - 127);
+    ring.isv[slot * 8 + grp] = __uint_as_float((uint32_t)(254 - ev) << 23);
+    if (bits) atomicOr(&s_bad[grp >> 1], bits << (16 * (grp & 1)));
+  }
+}
+
+// Scores of 32 columns whose bit is not set become -inf.
+__device__ __noinline__ void mask_scores(uint32_t addr, uint32_t word) {
+  uint32_t x[32];
+  tmem_ld32(addr, x);
+#pragma unroll
+  for (int e = 0; e < 32; ++e)
+    if (!((word >> e) & 1u)) x[e] = 0xff800000u;
+  tmem_st32(addr, x);
+  tmem_wait_st();
+}
+
+template <int D>
+__global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttnParams p, const __grid_constant__ CUtensorMap kmap,
+                                                                 const __grid_constant__ CUtensorMap vmap, const int box_rows) {
+  constexpr int TILE8 = TC_BN * D;      // 128 rows of codes
+  constexpr int TILE = 2 * TILE8;       // 128 rows of fp16
   extern __shared__ uint8_t smem_raw[];
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   uint32_t* s_anc = reinterpret_cast<uint32_t*>(base);               // 2048 B
@@ -85,20 +294,30 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   uint64_t* s_bar = reinterpret_cast<uint64_t*>(base + 3072);        // QB_COUNT * 8
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(base + 3328);
   volatile int* s_abort = reinterpret_cast<volatile int*>(base + 3332);   // [0] a wait gave up; [1] the same for the last wait
-  uint32_t* s_bad = reinterpret_cast<uint32_t*>(base + 3344);          // [4]: node rows with a NaN or an infinity
+  uint32_t* s_bad = reinterpret_cast<uint32_t*>(base + 3344);        // [4]: node rows with a NaN or an infinity
+  uint32_t* s_flag = reinterpret_cast<uint32_t*>(base + 3360);       // [4 slots]: 16-key groups of a block with a NaN scale
   float* s_ks = reinterpret_cast<float*>(base + 3392);               // [4 slots][8 groups of 16 keys] K scale
   float* s_lsv = s_ks + 32;                                          // log2 of the V scale
   float* s_isv = s_lsv + 32;                                         // 1 / V scale
   float* s_qs = reinterpret_cast<float*>(base + 3840);               // [256 rows] scale of a Q row
-  float* s_ml = reinterpret_cast<float*>(base + 4864);               // [2][128] reference and sum of stream 1 (mode B)
-  uint8_t* sQ = base + QT_SMALL;
-  uint8_t* sK = sQ + 2 * TILE;
-  uint8_t* sV = sK + 2 * TILE;
+  float* s_ml = reinterpret_cast<float*>(base + 4864);               // [2 streams][reference, sum][128]
+  uint8_t* sQ = base + QT_SMALL;      // [2 tiles][2 terms]
+  uint8_t* sK = sQ + 4 * TILE8;       // [2 stages] codes
+  uint8_t* sK2 = sK + 2 * TILE8;      // second term of the tree's K
+  uint8_t* sVr = sK2 + TILE8;         // [2 stages] codes
+  uint8_t* sV = sVr + 2 * TILE8;      // [2 stages] fp16
 
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;  // (known to be uniform)
   const int split = blockIdx.x;
   const int Hq = p.tree.n_q_heads, Hkv = p.kv.n_kv_heads, G = p.G;
-  if (warp == QT_CVT_WARP) {
+  if (tid == 0) {
+    s_abort[0] = s_abort[1] = 0;
+    for (int i = 0; i < 4; ++i) s_bad[i] = s_flag[i] = 0;
+    for (int i = 0; i < QB_COUNT; ++i)
+      mbar_init(&s_bar[i], i <= QB_P_FULL11 ? 128 : i <= QB_VR_EMPTY1 ? 2 : i == QB_Q_FULL ? QT_SOFTMAX : 1);
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == QT_MMA_WARP) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(s_tmem)), "r"(QT_TMEM_COLS));
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::);
   }
@@ -120,22 +339,11 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       const bool pages_ok = si.err ? true : quant_pages_in_pool(p.kv, b, si.P, whole_cta());
       if (tid == 0) p.status[b] = si.err ? si.err : (pages_ok ? 0 : (int)SB_ERR_BOUNDS);
     }
-    if (warp == QT_CVT_WARP)
+    if (warp == QT_MMA_WARP)
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(*s_tmem), "r"(QT_TMEM_COLS));
     return;
   }
   const bool two = row0 + TC_BM < rows_total;   // mode A
-  if (tid == 0) {
-    s_abort[0] = s_abort[1] = 0;
-    for (int i = 0; i < 4; ++i) s_bad[i] = 0;
-    for (int i = 0; i < QB_COUNT; ++i) {
-      const bool full = i == QB_K_FULL0 || i == QB_K_FULL1 || i == QB_V_FULL0 || i == QB_V_FULL1 || (i >= QB_SC0 && i <= QB_SC3);
-      const bool empty = i == QB_K_EMPTY0 || i == QB_K_EMPTY1 || i == QB_V_EMPTY0 || i == QB_V_EMPTY1;
-      mbar_init(&s_bar[i], full ? 4 : empty && two ? 2 : 1);  // a stage is free when its last reader, of one or two streams, is done
-    }
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-  }
-  __syncthreads();
   const long long rows_all = (long long)p.total_q * Hq;
 
   const BlockList list = visible_blocks(si.P, p.window, p.sinks, TC_BN);
@@ -143,43 +351,57 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   const int per = total / p.num_splits, rem = total % p.num_splits;
   const int blk0 = split * per + min(split, rem);
   const int nb = per + (split < rem ? 1 : 0);
-  const int nv = two ? 2 * nb : nb;
-  const uint32_t tmem = *s_tmem;
-  const uint32_t tmem_o = tmem + 2 * TC_BN;
+  const int steps = two ? 2 * nb : nb;                              // of 64 keys, for each stream
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *s_tmem, 0);
+  const uint32_t tmem_o = tmem + 4 * 64;                            // accumulator of stream t at tmem_o + t * D
 
   // state of the softmax threads
   const int t_mine = warp >> 2, row = (warp & 3) * 32 + lane;
   const uint32_t lane_base = ((uint32_t)((warp & 3) * 32)) << 16;
   float ref = 0.f, l_run = 0.f;
-  bool seen_any = false, ok = true, compute = false;
+  bool seen_any = false;  // the row has met a visible key, and `ref` is its reference
+  bool ok = true, compute = false;
 
-  if (tid < QT_SOFTMAX) {
-    // ---- Q: 16-byte pieces, D / 8 lanes to a row ---------------------------------------------------------------
-    constexpr int LPR = D / 8, RPP = QT_SOFTMAX / LPR;
-    const int n_rows = two ? 2 * TC_BM : TC_BM;
-#pragma unroll 4
-    for (int r0 = 0; r0 < n_rows; r0 += RPP) {
-      const int r = r0 + tid / LPR, ch = tid % LPR;
-      const int R = row0 + r;
-      const int nl = R / G;
-      const bool on = R < rows_total && SB_CHECKED_ACCESS(si.q_off + nl, p.total_q, &p.status[b]);
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (on) v = *reinterpret_cast<const uint4*>(p.q + (long long)(si.q_off + nl) * p.q_stride + (long long)(g * G + R - nl * G) * D + ch * 8);
-      uint32_t w[4] = {v.x, v.y, v.z, v.w};
-      uint32_t amax = 0;
+  if (warp < QT_SOFTMAX / 32) {
+    // ---- Q: 16-byte pieces, D / 8 lanes to a row, eight loads in flight -----------------------------------------------
+    constexpr int LPR = D / 8, RPP = QT_SOFTMAX / LPR, BATCH = 8;
+    const int n_rows = two ? 2 * TC_BM : TC_BM, ch = tid % LPR;
+#pragma unroll 1
+    for (int r0 = 0; r0 < n_rows; r0 += BATCH * RPP) {
+      uint4 x[BATCH];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) amax = max(amax, max(w[k] & 0x7FFFu, (w[k] >> 16) & 0x7FFFu));
+      for (int i = 0; i < BATCH; ++i) {
+        const int R = row0 + r0 + i * RPP + tid / LPR, Rc = R < rows_total ? R : 0;
+        const int nl = Rc / G;
+        const bool on = R < rows_total && SB_CHECKED_ACCESS(si.q_off + nl, p.total_q, &p.status[b]);
+        x[i] = __ldg(reinterpret_cast<const uint4*>(p.q + (long long)(si.q_off + (on ? nl : 0)) * p.q_stride +
+                                                    (long long)(g * G + Rc - nl * G) * D + ch * 8));
+        if (!on) x[i] = make_uint4(0, 0, 0, 0);
+      }
 #pragma unroll
-      for (int d = 1; d < LPR; d <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, d));
-      const int ex = (int)(amax >> 7);
-      const int e = ex == 0 || ex == 255 ? 127 : min(ex, 253);
-      const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
+      for (int i = 0; i < BATCH; ++i) {
+        const int r = r0 + i * RPP + tid / LPR;
+        uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+        uint32_t amax = 0;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) w[k] = pack_f16(__uint_as_float(w[k] << 16) * inv, __uint_as_float(w[k] & 0xFFFF0000u) * inv);
-      *reinterpret_cast<uint4*>(sQ + (r / TC_BM) * TILE + sw128_chunk_off(r % TC_BM, ch, TC_BM)) = make_uint4(w[0], w[1], w[2], w[3]);
-      if (ch == 0) s_qs[r] = __uint_as_float((uint32_t)e << 23) * p.scale_log2;
+        for (int k = 0; k < 4; ++k) amax = max(amax, max(w[k] & 0x7FFFu, (w[k] >> 16) & 0x7FFFu));
+#pragma unroll
+        for (int d = 1; d < LPR; d <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, d));
+        const int ex = (int)(amax >> 7);
+        const int e = ex == 255 ? 127 : min(max(ex - 7, 1), 253);   // the largest element becomes 2^7 .. 2^8
+        const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
+        uint16_t hi[4], lo[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) split_e4m3(__uint_as_float(w[k] << 16) * inv, __uint_as_float(w[k] & 0xFFFF0000u) * inv, hi[k], lo[k]);
+        uint8_t* dst = sQ + (r / TC_BM) * (2 * TILE8) + code_tile_off<D>(r % TC_BM, ch >> 1) + (ch & 1) * 8;
+        *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0] | ((uint32_t)hi[1] << 16), hi[2] | ((uint32_t)hi[3] << 16));
+        *reinterpret_cast<uint2*>(dst + TILE8) = make_uint2(lo[0] | ((uint32_t)lo[1] << 16), lo[2] | ((uint32_t)lo[3] << 16));
+        // a row with a NaN or an infinity is NaN throughout (e4m3 has no infinity)
+        if (ch == 0) s_qs[r] = ex == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)e << 23) * p.scale_log2;
+      }
     }
     fence_async_smem();
+    mbar_arrive(&s_bar[QB_Q_FULL]);
     const ThreadGroup grp = first_threads(QT_SOFTMAX);
     const bool tree_ok = build_ancestors_smem(p.tree.parent + si.node_base, si.err ? 0 : si.n, s_parent, s_anc, s_depth, grp);
     int err = si.err;
@@ -195,380 +417,326 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     const int node = (R < rows_total && compute) ? si.q0 + R / G : -1;
     const int pos = si.P + (node >= 0 ? s_depth[node] : 0);
     const float qs = s_qs[(two ? t_mine * TC_BM : 0) + row];
-    const uint32_t s_addr = tmem + lane_base + t_mine * TC_BN;
     bool poison = false;
 
-    const bool leader = (tid & 127) == 0;     // issues the MMAs of its stream
-    const uint32_t hi = tc_desc_hi(1024);
-    const uint32_t q_lo = tc_desc_lo(smem_u32(sQ) + (two ? t_mine * TILE : 0), 16), k_lo = tc_desc_lo(smem_u32(sK), 16);
-    const uint32_t v_lo = tc_desc_lo(smem_u32(sV), TC_BN * 128);
-    auto issue_s = [&](int n) {               // S of this stream's n-th block
-      const int j = two ? n : 2 * n + t_mine;
-      if (ok) ok = mbar_wait(&s_bar[QB_K_FULL0 + (j & 1)], (j >> 1) & 1, s_abort);
-      if (!ok) return;
-      tc_fence_after();
-      const uint32_t kb = k_lo + (j & 1) * (TILE >> 4), idesc = tc_idesc_f16(TC_BM, TC_BN, 0);
-#pragma unroll
-      for (int ks = 0; ks < D / 16; ++ks) {
-        const uint32_t koff = ((ks >> 2) * (TC_BM * 128) + (ks & 3) * 32) >> 4;
-        tc_mma_h(tmem + t_mine * TC_BN, q_lo + koff, kb + koff, hi, idesc, ks > 0);
-      }
-      tc_commit(&s_bar[QB_S_FULL0 + t_mine]);
-      tc_commit(&s_bar[QB_K_EMPTY0 + (j & 1)]);
-    };
-    auto issue_pv = [&](int n) {
-      const int j = two ? n : 2 * n + t_mine;
-      if (ok) ok = mbar_wait(&s_bar[QB_V_FULL0 + (j & 1)], (j >> 1) & 1, s_abort);
-      if (!ok) return;
-      tc_fence_after();
-      const uint32_t vb = v_lo + (j & 1) * (TILE >> 4), pb = tmem + t_mine * TC_BN, idesc = tc_idesc_f16(TC_BM, D, 1);
-#pragma unroll
-      for (int ks = 0; ks < TC_BN / 16; ++ks)
-        tc_mma_ts_h(tmem_o + t_mine * D, pb + ks * 8, vb + ks * (2048 >> 4), hi, idesc, (n > 0 || ks > 0) ? 1u : 0u);
-      tc_commit(&s_bar[QB_V_EMPTY0 + (j & 1)]);
-    };
-    const int my_blocks = nv > t_mine ? (nv - t_mine + 1) / 2 : 0;
-    if (leader && my_blocks > 0) issue_s(0);
-    // A wait that gives up leaves `ok` false; the loop still runs to its end, so that the warpgroup's barriers match.
-    for (int n = 0; n < my_blocks; ++n) {
-      const int v = 2 * n + t_mine;
-      const int j = two ? n : v;
-      const int at = blk0 + j, slot = (j & 3) * 8;
-      const bool is_tree = at >= list.count;
-      const int k0 = is_tree ? 0 : list.at(at) * TC_BN;
-      // blocks that every row sees whole need no mask
-      const bool masked = is_tree || k0 + TC_BN > si.P ||
-                          (p.window > 0 && k0 + TC_BN > p.sinks && si.P + si.n - 1 - k0 >= p.window);
-      if (ok) ok = mbar_wait(&s_bar[QB_SC0 + (j & 3)], (j >> 2) & 1, s_abort) && mbar_wait(&s_bar[QB_S_FULL0 + t_mine], n & 1, s_abort);
-      __syncwarp();
-      tc_fence_after();
-      uint32_t sr[2][32];
-      tmem_ld32_async(s_addr, sr[0]);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint32_t(&x)[32] = sr[q & 1];
-        tmem_wait_ld(x);
-        if (q < 3) tmem_ld32_async(s_addr + 32 * (q + 1), sr[(q + 1) & 1]);
-        const float2 ks = *reinterpret_cast<const float2*>(s_ks + slot + 2 * q);
-        const float2 lsv = *reinterpret_cast<const float2*>(s_lsv + slot + 2 * q);
-        const float2 isv = *reinterpret_cast<const float2*>(s_isv + slot + 2 * q);
+    // One step's 64 scores of this row -> probabilities, 32 columns at a time, the next 32 in flight.  (Rolled: unrolled twice, the
+    // kernel outgrows the instruction caches.)
+    auto walk = [&](int i, int group, uint32_t s_addr) {
+      uint32_t x[32];
+      tmem_ld32_async(s_addr, x);
+#pragma unroll 1
+      for (int q = 0; q < 2; ++q) {
+        const float2 ks = *reinterpret_cast<const float2*>(s_ks + group + 2 * q);
+        const float2 ls = *reinterpret_cast<const float2*>(s_lsv + group + 2 * q);
+        const float2 is = *reinterpret_cast<const float2*>(s_isv + group + 2 * q);
         // exponents relative to the present reference
-        const float f0 = qs * ks.x, f1 = qs * ks.y, c0 = lsv.x - ref, c1 = lsv.y - ref;
-        unsigned long long mul[2] = {pack_f32x2(f0, f0), pack_f32x2(f1, f1)}, add[2] = {pack_f32x2(c0, c0), pack_f32x2(c1, c1)};
+        const float f0 = qs * ks.x, f1 = qs * ks.y, c0 = ls.x - ref, c1 = ls.y - ref;
+        const unsigned long long mul[2] = {pack_f32x2(f0, f0), pack_f32x2(f1, f1)}, add[2] = {pack_f32x2(c0, c0), pack_f32x2(c1, c1)};
+        tmem_wait_ld(x);
         float d[32];
 #pragma unroll
-        for (int i = 0; i < 32; i += 2)
-          unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), mul[i >> 4], add[i >> 4]), d[i], d[i + 1]);
-        if (masked) {
+        for (int e = 0; e < 32; e += 2)
+          unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), mul[e >> 4], add[e >> 4]), d[e], d[e + 1]);
+        if (q == 0) tmem_ld32_async(s_addr + 32, x);
+        // The reference stays while no exponent is far above it.  That shows in the sum, which is needed anyway: a sum
+        // beyond 2^13 (or infinite) means an exponent above 8, and the 32 columns are done again with a new reference.
+        uint32_t pk[16];
+        float a0, b0;
+        bool raise = !seen_any;
+        while (true) {
+          if (__any_sync(0xffffffffu, raise)) {
+            float top = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) top = max3(top, d[e], d[e + 1]);
+            const float delta = raise && top > -INFINITY ? top : 0.f;
+            const float factor = seen_any ? fast_exp2(-delta) : 1.f;  // nothing accumulated yet: nothing to scale
+            seen_any |= raise && top > -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) d[e] -= delta;
+            ref += delta;
+            l_run *= factor;
+            // the accumulator holds the steps before this one: the last of them may still be under way
+            if (i > 0) {
+              if (ok) ok = mbar_wait(&s_bar[QB_PV0 + t_mine], (i - 1) & 1, s_abort);
+              __syncwarp();
+              tc_fence_after();
+            }
+            rescale_row<D>(i > 0 ? tmem_o + t_mine * D + lane_base : 0xffffffffu, s_addr, q, factor);
+          }
+          unsigned long long sum2[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
+#pragma unroll
+          for (int e = 0; e < 32; e += 2) {
+            const float p0 = fast_exp2(d[e]), p1 = fast_exp2(d[e + 1]);
+            sum2[e >> 4] = add_f32x2(sum2[e >> 4], pack_f32x2(p0, p1));
+            pk[e >> 1] = pack_f16(p0, p1);
+          }
+          float a1, b1;
+          unpack_f32x2(sum2[0], a0, a1);
+          unpack_f32x2(sum2[1], b0, b1);
+          a0 += a1;
+          b0 += b1;
+          raise = a0 + b0 > kQuantLimit;
+          if (!__any_sync(0xffffffffu, raise)) break;
+        }
+        l_run = fmaf(b0, is.y, fmaf(a0, is.x, l_run));
+        tmem_st16(s_addr + 16 * q, pk);
+      }
+    };
+    // A wait that gives up leaves `ok` false; the loop still runs to its end, so that every barrier gets its arrivals.
+    for (int i = 0; i < steps; ++i) {
+      const int j = two ? i >> 1 : i, half = two ? i & 1 : t_mine;
+      const int at = blk0 + j, group = (j & 3) * 8 + half * 4;
+      const bool is_tree = at >= list.count;
+      const int k0 = (is_tree ? 0 : list.at(at) * TC_BN) + 64 * half;
+      // steps that every row sees whole need no mask
+      const bool masked = is_tree || k0 + 64 > si.P || (p.window > 0 && k0 + 64 > p.sinks && si.P + si.n - 1 - k0 >= p.window);
+      if (ok) ok = mbar_wait(&s_bar[QB_SC0 + (j & 3)], (j >> 2) & 1, s_abort) &&
+                   mbar_wait(&s_bar[QB_S_FULL00 + 2 * t_mine + (i & 1)], (i >> 1) & 1, s_abort);
+      __syncwarp();
+      tc_fence_after();
+      const uint32_t s_addr = tmem + lane_base + (2 * t_mine + (i & 1)) * 64;
+      const uint32_t flags = is_tree ? 0u : (s_flag[j & 3] >> (4 * half)) & 15u;   // poisoned 16-key groups of the step
+      if (masked || flags) {
+        // invisible scores become -inf in tensor memory before the walk
+#pragma unroll 1
+        for (int q = 0; q < 2; ++q) {
           uint32_t word;
           if (is_tree) {
-            word = node >= 0 ? s_anc[4 * node + q] : 0u;
+            const int w0 = (k0 >> 5) + q;    // k0: first node of the step
+            word = node >= 0 ? s_anc[4 * node + w0] : 0u;
             if (p.window > 0) {
               for (uint32_t w = word; w; w &= w - 1) {
-                const int bit = __ffs(w) - 1, kp = si.P + s_depth[32 * q + bit];
+                const int bit = __ffs(w) - 1, kp = si.P + s_depth[32 * w0 + bit];
                 if (!(kp < p.sinks || pos - kp < p.window)) word &= ~(1u << bit);
               }
             }
-            poison |= (word & s_bad[q]) != 0;
+            poison |= (word & s_bad[w0]) != 0;
           } else {
             const int kq = k0 + 32 * q;
             word = low_bits(si.P - kq);
             if (p.window > 0) word &= low_bits(p.sinks - kq) | ~low_bits(pos - p.window + 1 - kq);
+            poison |= ((flags >> (2 * q)) & 1u && (word & 0xFFFFu)) || ((flags >> (2 * q + 1)) & 1u && (word >> 16));
           }
-#pragma unroll
-          for (int i = 0; i < 32; ++i)
-            if (!((word >> i) & 1u)) d[i] = -INFINITY;
+          mask_scores(s_addr + 32 * q, word);
         }
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 32; i += 2) top = max3(top, d[i], d[i + 1]);
-        const bool step = seen_any ? top > kQuantStep : top > -INFINITY;
-        if (__any_sync(0xffffffffu, step)) {
-          const float delta = step ? top : 0.f;
-          const float factor = step && seen_any ? fast_exp2(-delta) : 1.f;
-#pragma unroll
-          for (int i = 0; i < 32; ++i) d[i] -= delta;
-          ref += delta;
-          l_run *= factor;
-          seen_any |= step;
-          if (n > 0) {  // PV of this stream's previous block is complete (see above)
-#pragma unroll 1
-            for (int c = 0; c < D / 16; ++c) {
-              uint32_t r[16];
-              tmem_ld16(tmem_o + t_mine * D + lane_base + c * 16, r);
-#pragma unroll
-              for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * factor);
-              tmem_st16(tmem_o + t_mine * D + lane_base + c * 16, r);
-            }
-          }
-          if (q > 0) tmem_wait_st();  // the quarters already written are read back
-#pragma unroll 1
-          for (int c = 0; c < q; ++c) {
-            uint32_t r[16];
-            tmem_ld16(s_addr + 16 * c, r);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r[i]));
-              r[i] = pack_f16(f.x * factor, f.y * factor);
-            }
-            tmem_st16(s_addr + 16 * c, r);
-          }
-          tmem_wait_st();
-        }
-        uint32_t pk[16];
-        unsigned long long sum2[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
-#pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-          const float p0 = fast_exp2(d[i]), p1 = fast_exp2(d[i + 1]);
-          sum2[i >> 4] = add_f32x2(sum2[i >> 4], pack_f32x2(p0, p1));
-          pk[i >> 1] = pack_f16(p0, p1);
-        }
-        float a0, a1, b0, b1;
-        unpack_f32x2(sum2[0], a0, a1);
-        unpack_f32x2(sum2[1], b0, b1);
-        a0 += a1;
-        b0 += b1;
-        if (a0 != 0.f) l_run = fmaf(a0, isv.x, l_run);  // a NaN scale must not meet an empty group
-        if (b0 != 0.f) l_run = fmaf(b0, isv.y, l_run);
-        tmem_st16(s_addr + 16 * q, pk);
       }
+      walk(i, group, s_addr);
       tmem_wait_st();
       tc_fence_before();
-      asm volatile("bar.sync %0, 128;" ::"r"(2 + t_mine) : "memory");
-      if (leader) {
-        issue_pv(n);
-        if (n + 1 < my_blocks) issue_s(n + 1);
-      }
-      __syncwarp();
+      mbar_arrive(&s_bar[QB_P_FULL00 + 2 * t_mine + (i & 1)]);
     }
-    if (leader) tc_commit(&s_bar[QB_O_DONE0 + t_mine]);
     if (!ok) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
     if (poison) l_run = __uint_as_float(0x7FC00000u);
     if (!compute) {
       l_run = 0.f;
       seen_any = false;
     }
-  } else {
-    // ---- converters ---------------------------------------------------------------------------------------------------
-    const int cw = warp - QT_CVT_WARP;          // rows [32 cw, 32 cw + 32) of every block
-    constexpr int CPR = D / 16, RPI = 32 / CPR, NI = 32 / RPI;
-    const int ch = lane % CPR, r_in = lane / CPR;
-    const long long width = (long long)Hkv * D;
-    long long half_row[2] = {0, 0};             // cache rows of this warp's two 16-key halves, of the block looked up last
-    int k0 = 0;
-    float ks_raw = 1.f, vs_raw = 1.f;           // lanes 0 and 1: scales of half `lane` of the block loaded last
-    bool v_zero[2] = {false, false};
-    uint4 kx[NI], vx[NI];
-    auto lookup = [&](int j) {
-      if (j >= nb || blk0 + j >= list.count) return;
-      k0 = list.at(blk0 + j) * TC_BN + 32 * cw;
-      half_row[0] = k0 < si.P ? quant_row(p.kv, b, k0) : 0;
-      half_row[1] = k0 + 16 < si.P ? quant_row(p.kv, b, k0 + 16) : 0;
-    };
-    auto load = [&](const uint8_t* codes, uint4 (&x)[NI]) {
+  } else if (warp == QT_MMA_WARP) {
+    // ---- MMA issuer -------------------------------------------------------------------------------------------------
+    const uint32_t elected = elect_one();
+    const uint32_t hi = tc_desc_hi(1024);
+    // 8-bit tiles: 128-byte rows and swizzle (eight rows = 1024 bytes), or 64-byte ones (512; layout type 4)
+    const uint32_t hi8 = D == 128 ? tc_desc_hi(1024) : ((512u >> 4) | (1u << 14) | (4u << 29));
+    const uint32_t q_lo = tc_desc_lo(smem_u32(sQ), 16), k_lo = tc_desc_lo(smem_u32(sK), 16), k2_lo = tc_desc_lo(smem_u32(sK2), 16);
+    const uint32_t v_lo = tc_desc_lo(smem_u32(sV), TC_BN * 128);
+    const uint32_t idesc_s = tc_idesc_e4m3(TC_BM, 64), idesc_pv = tc_idesc_f16(TC_BM, D, 1);
+    auto issue_s = [&](int t, int i) {
+      const int j = two ? i >> 1 : i, half = two ? i & 1 : t;
+      if (t == 0 && (!two || half == 0)) ok = ok && mbar_wait(&s_bar[QB_K_FULL0 + (j & 1)], (j >> 1) & 1, s_abort);  // first reader
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) return;
+      tc_fence_after();
+      const uint32_t qb = q_lo + (two ? t : 0) * (2 * TILE8 >> 4), d = tmem + (2 * t + (i & 1)) * 64;
+      uint32_t kb = k_lo + (j & 1) * (TILE8 >> 4) + half * (64 * D >> 4);
+      // (Q1 + Q2) K, and for the tree (Q1 + Q2) (K1 + K2); 32 elements a step
+      const int terms = blk0 + j >= list.count ? 2 : 1;
+#pragma unroll 1
+      for (int c = 0; c < terms; ++c) {
 #pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const int r = i * RPI + r_in;
-        const long long crow = (i * RPI < 16 ? half_row[0] : half_row[1]) + (r & 15);
-        x[i] = make_uint4(0, 0, 0, 0);
-        if (k0 + r < si.P && SB_CHECKED_ACCESS(crow, quant_rows_total(p.kv), &p.status[b]))
-          x[i] = __ldg(reinterpret_cast<const uint4*>(codes + crow * width + g * D + ch * 16));
+        for (int ks = 0; ks < D / 16; ++ks)
+          warp_mma_f8(elected, d, qb + (ks / (D / 32)) * (TILE8 >> 4) + (ks % (D / 32)) * 2, kb + (ks % (D / 32)) * 2, hi8, idesc_s, c + ks > 0);
+        kb = k2_lo + half * (64 * D >> 4);
       }
+      warp_commit(elected, &s_bar[QB_S_FULL00 + 2 * t + (i & 1)]);
+      if (t == 1 && (!two || half == 1)) warp_commit(elected, &s_bar[QB_K_EMPTY0 + (j & 1)]);                        // last reader
     };
-    auto load_scales = [&]() {
-      ks_raw = vs_raw = 1.f;
-      if (lane < 2 && k0 + 16 * lane < si.P) {
-        const long long off = (lane == 0 ? half_row[0] : half_row[1]) / p.kv.scale_block * Hkv + g;
-        ks_raw = p.k_scale[off];
-        vs_raw = p.v_scale[off];
-      }
+    auto issue_pv = [&](int t, int i) {
+      const int j = two ? i >> 1 : i, half = two ? i & 1 : t;
+      ok = ok && mbar_wait(&s_bar[QB_P_FULL00 + 2 * t + (i & 1)], (i >> 1) & 1, s_abort);
+      if (t == 0 && (!two || half == 0)) ok = ok && mbar_wait(&s_bar[QB_V_FULL0 + (j & 1)], (j >> 1) & 1, s_abort);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) return;
+      tc_fence_after();
+      const uint32_t vb = v_lo + (j & 1) * (TILE >> 4) + half * (4 * 2048 >> 4), pb = tmem + (2 * t + (i & 1)) * 64;
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+        warp_mma_ts(elected, tmem_o + t * D, pb + ks * 8, vb + ks * (2048 >> 4), hi, idesc_pv, (i > 0 || ks > 0) ? 1u : 0u);
+      warp_commit(elected, &s_bar[QB_PV0 + t]);
+      if (t == 1 && (!two || half == 1)) warp_commit(elected, &s_bar[QB_V_EMPTY0 + (j & 1)]);
     };
-    auto store_pair = [&](uint8_t* stage, int r, const uint4 (&h)[2]) {
-      // Two 16-byte chunks of one row.  D = 128: the lanes of a row's upper half, whose tile repeats the banks of the lower
-      // one, store them in the other order.
-      const bool swap = D == 128 && (lane & 4);
-      const uint4 a = swap ? h[1] : h[0], b2 = swap ? h[0] : h[1];
-      *reinterpret_cast<uint4*>(stage + sw128_chunk_off(r, 2 * ch + (swap ? 1 : 0), TC_BN)) = a;
-      *reinterpret_cast<uint4*>(stage + sw128_chunk_off(r, 2 * ch + (swap ? 0 : 1), TC_BN)) = b2;
-    };
-    auto convert = [&](uint8_t* stage, const uint4 (&x)[NI], bool z0, bool z1) {
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const bool z = i * RPI < 16 ? z0 : z1;
-        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-        uint32_t h[8];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          h[2 * k] = z ? 0u : half2_of_e4m3x2((uint16_t)w[k]);
-          h[2 * k + 1] = z ? 0u : half2_of_e4m3x2((uint16_t)(w[k] >> 16));
-        }
-        const uint4 o[2] = {make_uint4(h[0], h[1], h[2], h[3]), make_uint4(h[4], h[5], h[6], h[7])};
-        store_pair(stage, 32 * cw + i * RPI + r_in, o);
-      }
-    };
-    auto put_scales = [&](int j, float ks, float vs) {
-      const int at = (j & 3) * 8 + 2 * cw + lane;
-      s_ks[at] = ks;
-      s_lsv[at] = log2f(vs);
-      s_isv[at] = 1.f / vs;
-    };
-    auto publish = [&](uint64_t* bar) {
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar);
-    };
-    // The tree: bf16 rows -> fp16 with a power of two per 16 rows.  Rows that hold a NaN or an infinity become zeros.
-    auto node_rows = [&](const bf16* src, int half, uint4 (&x)[NI]) {  // x: this lane's 16 elements of NI / 2 rows
-#pragma unroll
-      for (int i = 0; i < NI / 2; ++i) {
-        const int nd = 32 * cw + 16 * half + i * RPI + r_in;
-        x[2 * i] = x[2 * i + 1] = make_uint4(0, 0, 0, 0);
-        if (nd < si.n && SB_CHECKED_ACCESS(si.node_base + nd, p.tree.total_nodes, &p.status[b])) {
-          const uint4* s4 = reinterpret_cast<const uint4*>(src + (long long)(si.node_base + nd) * p.node_stride + g * D + ch * 16);
-          x[2 * i] = s4[0];
-          x[2 * i + 1] = s4[1];
-        }
-      }
-    };
-    auto bad_rows = [&](uint4 (&x)[NI], int half) {  // bits (row of the warp) of rows with a NaN or an infinity, which are zeroed
-      uint32_t bits = 0;
-#pragma unroll
-      for (int i = 0; i < NI / 2; ++i) {
-        const uint32_t w[8] = {x[2 * i].x, x[2 * i].y, x[2 * i].z, x[2 * i].w, x[2 * i + 1].x, x[2 * i + 1].y, x[2 * i + 1].z, x[2 * i + 1].w};
-        bool nf = false;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) nf |= bf16x2_nonfinite(w[k]);
-        const uint32_t votes = __ballot_sync(0xffffffffu, nf);
-        const uint32_t mine = (votes >> (r_in * CPR)) & ((1u << CPR) - 1u);
-        if (mine) x[2 * i] = x[2 * i + 1] = make_uint4(0, 0, 0, 0);
-#pragma unroll
-        for (int r = 0; r < RPI; ++r)
-          if ((votes >> (r * CPR)) & ((1u << CPR) - 1u)) bits |= 1u << (16 * half + i * RPI + r);
-      }
-      return bits;
-    };
-    auto node_convert = [&](const bf16* src, uint8_t* stage, float (&scale)[2], bool is_v) {
-#pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        uint4 x[NI];
-        node_rows(src, half, x);
-        bad_rows(x, half);
-        uint32_t amax = 0;
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) amax = max(amax, max(w[k] & 0x7FFFu, (w[k] >> 16) & 0x7FFFu));
-        }
-        amax = __reduce_max_sync(0xffffffffu, amax);
-        int e = (int)(amax >> 7) - 8;              // biased exponent of the scale: the largest value becomes 2^8 .. 2^9
-        e = amax < 0x80u ? 127 : max(e, is_v ? 127 - 60 : 1);
-        e = min(e, 253);
-        scale[half] = __uint_as_float((uint32_t)e << 23);
-        const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
-#pragma unroll
-        for (int i = 0; i < NI / 2; ++i) {
-          uint4 o[2];
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const uint4 v = x[2 * i + k];
-            const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-            uint32_t h[4];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) h[c] = pack_f16(__uint_as_float(w[c] << 16) * inv, __uint_as_float(w[c] & 0xFFFF0000u) * inv);
-            o[k] = make_uint4(h[0], h[1], h[2], h[3]);
-          }
-          store_pair(stage, 32 * cw + 16 * half + i * RPI + r_in, o);
-        }
-      }
-    };
-    auto is_prefix = [&](int j) { return j < nb && blk0 + j < list.count; };
-    lookup(0);
-    if (is_prefix(0)) {
-      load(p.k_codes, kx);
-      load_scales();
-      load(p.v_codes, vx);
+    if (steps > 0) ok = __all_sync(0xffffffffu, mbar_wait(&s_bar[QB_Q_FULL], 0, s_abort));
+    // (the first two rounds only issue S; rolled, so that the code is there once)
+#pragma unroll 1
+    for (int it = -4; it < 2 * steps; ++it) {
+      const int i = it >> 1, t = it & 1;
+      if (i >= 0) issue_pv(t, i);
+      if (i + 2 < steps) issue_s(t, i + 2);
     }
-    for (int j = 0; j < nb && ok; ++j) {
-      uint8_t* ks_stage = sK + (j & 1) * TILE;
-      uint8_t* vs_stage = sV + (j & 1) * TILE;
-      const bool prefix = is_prefix(j);
-      const float ks = ks_raw, vs = vs_raw;
-      lookup(j + 1);
-      if (j >= 2) ok = mbar_wait(&s_bar[QB_K_EMPTY0 + (j & 1)], ((j >> 1) - 1) & 1, s_abort);
+    warp_commit(elected, &s_bar[QB_O_DONE]);
+    if (!ok && lane == 0) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
+  } else if (warp == QT_LOAD_WARP) {
+    // ---- loader: lane l < 8 looks after keys 16 l .. + 15 of every block -----------------------------------------------
+    const int n_cache = max(0, min(nb, list.count - blk0));   // the blocks before the tree
+    const bool paged = p.kv.page_size != 0;
+    const int page_shift = paged ? 31 - __clz(p.kv.page_size) : 31;
+    const int* table = paged ? p.kv.page_table + (long long)b * p.kv.max_pages : nullptr;
+    auto my_key = [&](int j) { return list.at(blk0 + j) * TC_BN + 16 * lane; };
+    auto my_page = [&](int j) {  // page id of this lane's keys, unchecked (nothing waits for it here)
+      if (!paged || lane >= 8 || j >= n_cache || my_key(j) >= si.P) return 0;
+      return __ldg(table + (my_key(j) >> page_shift));
+    };
+    int page = my_page(0);
+    for (int j = 0; j < n_cache; ++j) {
+      const int key = my_key(j);
+      const bool on = lane < 8 && key < si.P;
+      if (page < 0 || page >= p.kv.num_pages) page = 0;  // reported by the designated CTA; reads stay in the pool
+      const int in_page = paged ? key & (p.kv.page_size - 1) : key;
+      const long long crow = (paged ? (long long)page << page_shift : (long long)b * p.kv.kv_capacity) + in_page;
+      float ks = 1.f, vs = 1.f;
+      if (on && SB_CHECKED_ACCESS(crow + 15, quant_rows_total(p.kv), &p.status[b])) {
+        ks = __ldg(p.k_scale + (crow >> p.block_shift) * Hkv + g);
+        vs = __ldg(p.v_scale + (crow >> p.block_shift) * Hkv + g);
+      }
+      const bool piece = on && (16 * lane & (box_rows - 1)) == 0;     // this lane's keys begin a TMA box
+      const uint32_t pieces = __popc(__ballot_sync(0xffffffffu, piece));
+      const int c2 = in_page, c3 = paged ? page : b;
+      page = my_page(j + 1);
+      if (j >= 2) ok = ok && mbar_wait(&s_bar[QB_K_EMPTY0 + (j & 1)], ((j >> 1) - 1) & 1, s_abort);
+      ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      if (prefix) {
-        const uint32_t tiny = __ballot_sync(0xffffffffu, vs < kMinVScale);
-        v_zero[0] = tiny & 1;
-        v_zero[1] = (tiny >> 1) & 1;
-        if (lane < 2) put_scales(j, ks, v_scale_used(vs));
-        convert(ks_stage, kx, false, false);
-        publish(&s_bar[QB_K_FULL0 + (j & 1)]);
-        if (lane == 0) mbar_arrive(&s_bar[QB_SC0 + (j & 3)]);
-        if (is_prefix(j + 1)) {
-          load(p.k_codes, kx);
-          load_scales();
-        }
-        if (j >= 2) ok = mbar_wait(&s_bar[QB_V_EMPTY0 + (j & 1)], ((j >> 1) - 1) & 1, s_abort);
+      if (lane == 0) mbar_expect_tx(&s_bar[QB_K_FULL0 + (j & 1)], pieces * box_rows * D);
+      __syncwarp();
+      if (piece) tma_load_4d(smem_u32(sK) + (j & 1) * TILE8 + 16 * lane * D, &kmap, 0, g, c2, c3, &s_bar[QB_K_FULL0 + (j & 1)]);
+      if (j >= 2) ok = ok && mbar_wait(&s_bar[QB_VR_EMPTY0 + (j & 1)], ((j >> 1) - 1) & 1, s_abort);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      if (lane == 0) mbar_expect_tx(&s_bar[QB_VR_FULL0 + (j & 1)], pieces * box_rows * D);
+      __syncwarp();
+      if (piece) tma_load_4d(smem_u32(sVr) + (j & 1) * TILE8 + 16 * lane * D, &vmap, 0, g, c2, c3, &s_bar[QB_VR_FULL0 + (j & 1)]);
+      // A NaN scale poisons the rows that see one of its keys; it is noted, and 1 takes its place, so that it meets no other row.
+      const uint32_t nan = __ballot_sync(0xffffffffu, ks != ks || vs != vs), tiny = __ballot_sync(0xffffffffu, vs < kMinVScale);
+      if (ks != ks || vs != vs) ks = vs = 1.f;
+      vs = v_scale_used(vs);
+      if (lane < 8) {
+        const int at = (j & 3) * 8 + lane;
+        s_ks[at] = ks;
+        s_lsv[at] = log2_of_scale(vs);
+        s_isv[at] = __fdividef(1.f, vs);
+      }
+      if (lane == 0) s_flag[j & 3] = nan | (tiny << 8);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s_bar[QB_SC0 + (j & 3)]);
+    }
+    if (!ok && lane == 0) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
+  } else {
+    // ---- converters: warp cw owns rows 64 cw .. + 63 of every V block ----------------------------------------------------
+    const int cw = warp - QT_CVT_WARP, n_cache = max(0, min(nb, list.count - blk0));
+    constexpr int CPR = D / 16, RPI = 32 / CPR, NI = 32 / RPI;
+    const int ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
+    for (int j = 0; j < nb && ok; ++j) {
+      uint8_t* stage = sV + (j & 1) * TILE;
+      if (j < n_cache) {
+        ok = mbar_wait(&s_bar[QB_VR_FULL0 + (j & 1)], (j >> 1) & 1, s_abort) && mbar_wait(&s_bar[QB_SC0 + (j & 3)], (j >> 2) & 1, s_abort);
+        if (ok && j >= 2) ok = mbar_wait(&s_bar[QB_V_EMPTY0 + (j & 1)], ((j >> 1) - 1) & 1, s_abort);
+        ok = __all_sync(0xffffffffu, ok);
         if (!ok) break;
-        convert(vs_stage, vx, v_zero[0], v_zero[1]);
-        publish(&s_bar[QB_V_FULL0 + (j & 1)]);
-        if (is_prefix(j + 1)) load(p.v_codes, vx);
-      } else {
-        float kscale[2], vscale[2];
-        uint32_t bits = 0;
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        const uint8_t* raw = sVr + (j & 1) * TILE8;
+        const int left = si.P - list.at(blk0 + j) * TC_BN;
+        const uint32_t tiny = (s_flag[j & 3] >> 8) & 255u;
+#pragma unroll 1
+        for (int q = 0; q < 2; ++q) {
+          const int r0 = 64 * cw + 32 * q;
           uint4 x[NI];
-          node_rows(p.k_nodes, half, x);
-          bits |= bad_rows(x, half);
-        }
-        node_convert(p.k_nodes, ks_stage, kscale, false);
-        if (j >= 2) ok = mbar_wait(&s_bar[QB_V_EMPTY0 + (j & 1)], ((j >> 1) - 1) & 1, s_abort);
-        if (!ok) break;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          uint4 x[NI];
-          node_rows(p.v_nodes, half, x);
-          bits |= bad_rows(x, half);
+          for (int i = 0; i < NI; ++i) x[i] = *reinterpret_cast<const uint4*>(raw + code_tile_off<D>(r0 + i * RPI + r_in, ch));
+          if (left < r0 + 32 || tiny) {  // rows past the prefix (stale bytes), and blocks that read as zeros
+#pragma unroll
+            for (int i = 0; i < NI; ++i) {
+              const int r = r0 + i * RPI + r_in;
+              if (r >= left || ((tiny >> (r >> 4)) & 1u)) x[i] = make_uint4(0, 0, 0, 0);
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < NI; ++i) {
+            const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+            uint32_t h[8];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              h[2 * k] = half2_of_e4m3x2((uint16_t)w[k]);
+              h[2 * k + 1] = half2_of_e4m3x2((uint16_t)(w[k] >> 16));
+            }
+            const int r = r0 + i * RPI + r_in;
+            *reinterpret_cast<uint4*>(stage + sw128_chunk_off(r, 2 * ch, TC_BN)) = make_uint4(h[0], h[1], h[2], h[3]);
+            *reinterpret_cast<uint4*>(stage + sw128_chunk_off(r, 2 * ch + 1, TC_BN)) = make_uint4(h[4], h[5], h[6], h[7]);
+          }
         }
-        node_convert(p.v_nodes, vs_stage, vscale, true);
-        if (lane < 2) put_scales(j, lane == 0 ? kscale[0] : kscale[1], lane == 0 ? vscale[0] : vscale[1]);
-        if (lane == 0) s_bad[cw] = bits;
-        publish(&s_bar[QB_K_FULL0 + (j & 1)]);
+        fence_async_smem();
+        __syncwarp();
         if (lane == 0) {
+          mbar_arrive(&s_bar[QB_VR_EMPTY0 + (j & 1)]);
           mbar_arrive(&s_bar[QB_V_FULL0 + (j & 1)]);
-          mbar_arrive(&s_bar[QB_SC0 + (j & 3)]);
+        }
+      } else {  // the tree
+        const ScaleRing ring = {s_ks, s_lsv, s_isv, s_flag};
+        const long long first = (long long)si.node_base * p.node_stride + g * D;
+#pragma unroll 1
+        for (int side = 0; side < 2; ++side) {  // K, V
+          if (j >= 2) ok = ok && mbar_wait(&s_bar[(side ? QB_V_EMPTY0 : QB_K_EMPTY0) + (j & 1)], ((j >> 1) - 1) & 1, s_abort);
+          ok = __all_sync(0xffffffffu, ok);
+          if (ok)
+            for (int grp = 4 * cw; grp < 4 * cw + 4; ++grp)
+              node_group<D>(p.k_nodes + first, p.v_nodes + first, p.node_stride, si.n, grp, sK + (j & 1) * TILE8, sK2, side ? stage : nullptr,
+                            ring, j & 3, s_bad);
+          fence_async_smem();
+          asm volatile("bar.sync 2, 64;" ::: "memory");   // both converter warps
+          if (lane == 0 && ok) {
+            if (side) mbar_arrive(&s_bar[QB_V_FULL0 + (j & 1)]);
+            else if (cw == 0) {
+              mbar_arrive(&s_bar[QB_K_FULL0 + (j & 1)]);
+              mbar_arrive(&s_bar[QB_SC0 + (j & 3)]);
+            }
+          }
         }
       }
     }
-    if (!ok) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
+    if (!ok && lane == 0) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
   }
 
   // ---- store ----------------------------------------------------------------------------------------------------------
-  // One thread per row: normalised by its own sum.  In mode B the second stream hands its row over in shared memory.
+  // Every thread of a stream normalises its row and stages it as bf16 with the row's number and log-sum-exp (over the idle Q and K
+  // tiles); then half a warp per row writes whole rows.  In mode B the second stream first hands its row over.
+  constexpr int ROWB = D * 2 + 16;                    // [bf16 row | base-2 log-sum-exp | pad | global row or -1]
   const bool have = nb > 0;
-  if (tid < QT_SOFTMAX) {
+  if (warp < QT_SOFTMAX / 32) {
     // awaited even after a wait that gave up: tensor memory is idle before it is freed
-    if (!mbar_wait(&s_bar[QB_O_DONE0 + t_mine], 0, s_abort + 1)) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
+    if (!mbar_wait(&s_bar[QB_O_DONE], 0, s_abort + 1)) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
     __syncwarp();
     tc_fence_after();
     if (l_run != l_run) {  // a NaN outweighs everything it is merged with
       ref = INFINITY;
       seen_any = true;
     }
-    const int streams = two ? 1 : (nv > 1 ? 2 : 1);   // accumulators per row
-    constexpr int RS = D + 4;                         // floats per row handed over (over the idle K and V tiles)
-    float* hand = reinterpret_cast<float*>(sK);
-    softmax_group_sync();                             // the MMAs of both streams are done
-    if (streams == 2 && t_mine == 1) {
+    const bool merge = !two && have;                  // two accumulators per row
+    constexpr int RS = D + 4;                         // floats per row handed over, over the idle V tiles and the end of K
+    float* hand = reinterpret_cast<float*>(sV + 2 * TILE - 128 * RS * 4);
+    if (merge && t_mine == 1) {
 #pragma unroll 1
-      for (int c = 0; c < D / 16; ++c) {
-        uint32_t r[16];
-        tmem_ld16(tmem_o + D + lane_base + c * 16, r);
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t r[32];
+        tmem_ld32(tmem_o + D + lane_base + c * 32, r);
 #pragma unroll
-        for (int i = 0; i < 16; i += 4)
-          *reinterpret_cast<uint4*>(hand + row * RS + c * 16 + i) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
+        for (int i = 0; i < 32; i += 4)
+          *reinterpret_cast<uint4*>(hand + row * RS + c * 32 + i) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
       }
       s_ml[row] = seen_any ? ref : -INFINITY;
       s_ml[128 + row] = l_run;
@@ -576,7 +744,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     softmax_group_sync();
     if (two || t_mine == 0) {
       float m = seen_any ? ref : -INFINITY, w0 = 1.f, w1 = 0.f, l = l_run;
-      if (streams == 2) {
+      if (merge) {
         const float m1 = s_ml[row], l1 = s_ml[128 + row], M = fmaxf(m, m1);
         w0 = m == -INFINITY ? 0.f : fast_exp2(m - M);
         w1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - M);
@@ -591,47 +759,51 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       const float inv = empty ? 0.f : 1.f / l;
       w0 *= inv;
       w1 *= inv;
+      uint8_t* dst = sQ + (two ? t_mine * (TC_BM * ROWB) : 0) + row * ROWB;
 #pragma unroll 1
-      for (int c = 0; c < D / 16; ++c) {
-        float f[16];
-        if (have) {
-          uint32_t r[16];
-          tmem_ld16(tmem_o + (two ? t_mine * D : 0) + lane_base + c * 16, r);
+      for (int c = 0; c < D / 32; ++c) {
+        uint32_t r[32];
+        if (have) tmem_ld32(tmem_o + (two ? t_mine * D : 0) + lane_base + c * 32, r);
 #pragma unroll
-          for (int i = 0; i < 16; ++i) f[i] = w0 == 0.f ? 0.f : __uint_as_float(r[i]) * w0;
-          if (streams == 2 && w1 != 0.f)
+        for (int i = 0; i < 32; i += 8) {
+          float f[8];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) f[i] = fmaf(hand[row * RS + c * 16 + i], w1, f[i]);
-        } else {
+          for (int k = 0; k < 8; ++k) f[k] = have && w0 != 0.f ? __uint_as_float(r[i + k]) * w0 : 0.f;
+          if (w1 != 0.f)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) f[i] = 0.f;
-        }
-        if (!on) continue;
-        if (p.outer == 1) {
-          uint4* dst = reinterpret_cast<uint4*>(p.out + grow * D + c * 16);
-          dst[0] = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-          dst[1] = make_uint4(pack_bf16(f[8], f[9]), pack_bf16(f[10], f[11]), pack_bf16(f[12], f[13]), pack_bf16(f[14], f[15]));
-        } else {
-          float4* dst = reinterpret_cast<float4*>(p.part_o + ((long long)split * rows_all + grow) * D + c * 16);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) dst[i] = make_float4(f[4 * i], f[4 * i + 1], f[4 * i + 2], f[4 * i + 3]);
+            for (int k = 0; k < 8; ++k) f[k] = fmaf(hand[row * RS + c * 32 + i + k], w1, f[k]);
+          *reinterpret_cast<uint4*>(dst + (c * 32 + i) * 2) =
+              make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
         }
       }
-      if (on) {
-        const float lse2 = empty ? -INFINITY : m + log2f(l);
-        if (p.outer == 1) {
-          if (p.lse) p.lse[grow] = empty ? 0.f : lse2 * kLn2;
-        } else {
-          p.part_lse[(long long)split * rows_all + grow] = lse2;
-        }
-      }
+      *reinterpret_cast<float*>(dst + D * 2) = empty ? -INFINITY : m + log2f(l);
+      *reinterpret_cast<long long*>(dst + D * 2 + 8) = on ? grow : -1ll;
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == QT_CVT_WARP) {
+  if (warp == QT_MMA_WARP) {
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(QT_TMEM_COLS));
+  }
+  const int n_staged = two ? 2 * TC_BM : TC_BM, col8 = lane & 15;
+  if (col8 < D / 8) {
+#pragma unroll 4
+    for (int r = 2 * warp + (lane >> 4); r < n_staged; r += 2 * (QT_THREADS / 32)) {
+      const uint8_t* rowp = sQ + r * ROWB;
+      const long long grow = *reinterpret_cast<const long long*>(rowp + D * 2 + 8);
+      const float lse2 = *reinterpret_cast<const float*>(rowp + D * 2);
+      const uint4 raw = *reinterpret_cast<const uint4*>(rowp + col8 * 16);
+      if (grow < 0) continue;
+      if (p.outer == 1) {
+        *reinterpret_cast<uint4*>(p.out + grow * D + col8 * 8) = raw;
+        if (p.lse && col8 == 0) p.lse[grow] = lse2 == -INFINITY ? 0.f : lse2 * kLn2;
+      } else {  // the staged row is bf16 already: partials keep that width
+        bf16* po = reinterpret_cast<bf16*>(p.part_o) + ((long long)split * rows_all + grow) * D + col8 * 8;
+        *reinterpret_cast<uint4*>(po) = raw;
+        if (col8 == 0) p.part_lse[(long long)split * rows_all + grow] = lse2;
+      }
+    }
   }
 }
 
@@ -654,7 +826,23 @@ static sb_status launch_quant_tc_d(const QuantAttnParams& p, dim3 grid, cudaStre
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, quant_tc_kernel<D>, p) != cudaSuccess) {
+  // rank-4 view (d, KV head, row, page) of the codes; a contiguous cache is one "page" of kv_capacity rows per sequence
+  const int box_rows = p.kv.page_size == 0 || p.kv.page_size > TC_BN ? TC_BN : p.kv.page_size;
+  CUtensorMap kmap, vmap;
+  const uint8_t* codes[2] = {p.k_codes, p.v_codes};
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (!enc) return SB_ERR_CUDA;
+  for (int i = 0; i < 2; ++i) {
+    const cuuint64_t H = (cuuint64_t)p.kv.n_kv_heads, rows = (cuuint64_t)(p.kv.page_size == 0 ? p.kv.kv_capacity : p.kv.page_size);
+    const cuuint64_t dims[4] = {(cuuint64_t)D, H, rows, (cuuint64_t)(p.kv.page_size == 0 ? p.kv.batch : p.kv.num_pages)};
+    const cuuint64_t strides[3] = {(cuuint64_t)D, H * D, rows * H * D};
+    const cuuint32_t box[4] = {(cuuint32_t)D, 1, (cuuint32_t)box_rows, 1}, elem[4] = {1, 1, 1, 1};
+    if (enc(i ? &vmap : &kmap, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<uint8_t*>(codes[i]), dims, strides, box, elem,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return SB_ERR_UNSUPPORTED;  // an extent or stride beyond what a tensor map holds
+  }
+  if (cudaLaunchKernelEx(&cfg, quant_tc_kernel<D>, p, kmap, vmap, box_rows) != cudaSuccess) {
     cudaGetLastError();
     return SB_ERR_CUDA;
   }

@@ -11,10 +11,11 @@ namespace sb {
 // pool is read as page 0, so that no access leaves the pool.
 __device__ inline long long quant_row(const sb_quant_cache& kv, int b, int j) {
   if (kv.page_size == 0) return (long long)b * kv.kv_capacity + j;
-  const int lp = j / kv.page_size;
+  const int shift = 31 - __clz(kv.page_size);  // a power of two
+  const int lp = j >> shift;
   int page = kv.page_table[(long long)b * kv.max_pages + lp];
   if (page < 0 || page >= kv.num_pages) page = 0;
-  return (long long)page * kv.page_size + (j - lp * kv.page_size);
+  return ((long long)page << shift) + (j & (kv.page_size - 1));
 }
 __host__ __device__ inline long long quant_rows_total(const sb_quant_cache& kv) {
   return kv.page_size == 0 ? (long long)kv.batch * kv.kv_capacity : (long long)kv.num_pages * kv.page_size;
