@@ -7,14 +7,15 @@
 // the bottom, and dividing by it is exact: a code is rounded once, and a later growth of the scale moves
 // the older codes by whole exponents (they lose bits only below 2^-6).
 //
-// Bound by memory: 2 bytes read and 1 written per element.  One CTA owns one (block, head, K or V): the maximum
-// needs the whole block before the first code can be written, and 128 tokens x 128 elements are 64 values a
-// thread, which stay in registers between the two steps.  Elements past the new rows are never touched.
+// Bound by memory for prompts: 2 bytes read and 1 written per element.  A unit of work is one (block, head, K or V): the maximum
+// needs the whole block before the first code can be written, so the new rows stay in registers between the two
+// steps, 64 elements a thread.  Prompts: one CTA of 2 * scale_block threads per unit, so that many small CTAs hide one
+// another's chain of dependent loads (lengths, rows and page ids, old scale).  Up to 16 rows (a verified step): one warp per
+// unit, eight to a CTA; there the chain is all there is, and a commit has thousands of units of a few hundred bytes.
+// Row loads go out before the page ids are looked at.  Elements past the new rows are never touched.
 #include "quant_common.cuh"
 
 namespace sb {
-
-constexpr int AP_THREADS = 256;
 
 struct AppendParams {
   sb_quant_cache kv;
@@ -25,6 +26,7 @@ struct AppendParams {
   const int* path_nodes;
   const int* accept_len;
   int max_depth, max_rows;
+  int block_shift;          // log2 of the tokens per block
   const int* len;
   int* new_len;
   int* status;
@@ -37,93 +39,152 @@ __device__ inline int scale_exponent(uint32_t amax_bits) {
   return e < -100 ? -100 : e;
 }
 
-template <int D>
-__global__ void __launch_bounds__(AP_THREADS) kv_append_quant_kernel(const AppendParams p) {
+// Eight bf16 values times a factor (or over a divisor) -> eight codes.
+__device__ inline uint2 codes_times(const uint4& x, float f) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t c[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) c[k] = e4m3x2_of(__uint_as_float(w[k] << 16) * f, __uint_as_float(w[k] & 0xFFFF0000u) * f);
+  return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+}
+__device__ __noinline__ uint2 codes_over(uint4 x, float s) {
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t c[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) c[k] = e4m3x2_of(__uint_as_float(w[k] << 16) / s, __uint_as_float(w[k] & 0xFFFF0000u) / s);
+  return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+}
+// Eight codes under another scale.
+__device__ __noinline__ uint2 rescaled(uint2 v, float old, float s) {
+  const uint32_t w[2] = {v.x, v.y};
+  uint32_t out[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const float2 a = float2_of_e4m3x2((uint16_t)w[k]), b = float2_of_e4m3x2((uint16_t)(w[k] >> 16));
+    out[k] = e4m3x2_of(a.x * old / s, a.y * old / s) | ((uint32_t)e4m3x2_of(b.x * old / s, b.y * old / s) << 16);
+  }
+  return make_uint2(out[0], out[1]);
+}
+
+// UT threads to a unit: a whole CTA, or one warp of a CTA of eight (UT = 32).
+template <int D, int UT>
+__global__ void __launch_bounds__(UT == 32 ? 256 : UT, UT == 32 ? 4 : 1152 / UT) kv_append_quant_kernel(const AppendParams p) {
   constexpr int LPR = D / 8;              // lanes per row: 8 elements (16 bytes of bf16) each
-  constexpr int RPP = AP_THREADS / LPR;   // rows per pass
-  constexpr int PASSES = 128 / RPP;
-  __shared__ int s_path[SB_MAX_DEPTH + 1];
-  __shared__ int s_err;
-  __shared__ uint32_t s_max[AP_THREADS / 32];
+  constexpr int RPP = UT / LPR;           // rows per pass
+  constexpr int ROWS = UT == 32 ? 16 : UT / 2;
+  constexpr int PASSES = ROWS / RPP;
+  constexpr int UNITS = UT == 32 ? 8 : 1;
+  __shared__ int s_path[UNITS][SB_MAX_DEPTH + 1];
+  __shared__ uint32_t s_max[UT == 32 ? 1 : UT / 32];
+  auto sync = []() {
+    if (UT == 32) __syncwarp();
+    else __syncthreads();
+  };
+  // the same value in every thread of the unit
+  auto any = [](bool v) { return UT == 32 ? __any_sync(0xffffffffu, v) != 0 : __syncthreads_or(v) != 0; };
   pdl_wait();
   pdl_release();
   const int H = p.kv.n_kv_heads, sb = p.kv.scale_block;
-  const int tid = threadIdx.x;
-  const int b = blockIdx.z % p.kv.batch, layer = blockIdx.z / p.kv.batch;
-  const int which = blockIdx.y & 1, g = blockIdx.y >> 1;
+  const int tid = threadIdx.x % UT, slot = threadIdx.x / UT;
+  const int b = blockIdx.y, layer = blockIdx.z;
+  const int unit = blockIdx.x * UNITS + slot, which = unit & 1, g = (unit >> 1) % H, nth = (unit >> 1) / H;
   const int start = p.len[b];
   const int o = p.row_offsets[b];
   const int avail = p.row_offsets[b + 1] - o;
-  int n = p.path_nodes ? p.accept_len[b] + 1 : avail;
+  const int n = p.path_nodes ? p.accept_len[b] + 1 : avail;
   int err = 0;
   if (o < 0 || avail < 0 || (long long)o + avail > p.total_rows || n < 0 || n > p.max_rows ||
       (p.path_nodes && (n < 1 || n > p.max_depth + 1)))
     err = SB_ERR_INVALID_TREE;
   const long long cap = p.kv.page_size == 0 ? p.kv.kv_capacity : (long long)p.kv.max_pages * p.kv.page_size;
   if (!err && (start < 0 || (long long)start + n > cap)) err = SB_ERR_BOUNDS;
-  if (tid == 0) s_err = err;
-  __syncthreads();
-  if (!err) {
-    if (p.path_nodes && tid < n) {
-      const int* path = p.path_nodes + (long long)b * (p.max_depth + 1);
-      const int self = path[tid];
-      s_path[tid] = self;
-      if (self < 0 || self >= avail || (tid > 0 && path[tid - 1] >= self)) s_err = SB_ERR_INVALID_TREE;
+  const bool first_unit = unit == 0 && layer == 0;
+  const int block = err ? 0 : (start >> p.block_shift) + nth; // block of tokens of this sequence
+  const long long t0 = (long long)block << p.block_shift;
+  const bool mine = !err && t0 < (long long)start + n;
+  if (!mine && !first_unit) return;                           // (the first unit has the sequence's status to write)
+  if (!err && p.path_nodes) {
+    const int* path = p.path_nodes + (long long)b * (p.max_depth + 1);
+    bool bad = false;
+    for (int i = tid; i < n; i += UT) {
+      const int self = path[i];
+      s_path[slot][i] = self;
+      bad |= self < 0 || self >= avail || (i > 0 && path[i - 1] >= self);
     }
-    if (p.kv.page_size > 0 && n > 0) {
-      const int first = start / p.kv.page_size, last = (start + n - 1) / p.kv.page_size;
-      for (int lp = first + tid; lp <= last; lp += AP_THREADS) {
-        const int page = p.kv.page_table[(long long)b * p.kv.max_pages + lp];
-        if (page < 0 || page >= p.kv.num_pages) atomicMax(&s_err, (int)SB_ERR_BOUNDS);
+    if (any(bad)) err = SB_ERR_INVALID_TREE;                  // (also a barrier: s_path is complete)
+  }
+  const int lo = (int)(t0 > start ? t0 : start) - (int)t0;    // new rows of the block: [lo, hi)
+  const int hi = mine ? (int)min((long long)start + n - t0, (long long)sb) : 0;
+  const int r_in = tid / LPR, col = (tid % LPR) * 8;
+  // Registers hold rows base + i * RPP + r_in; a warp's 16 rows start at the first new one.
+  const int base = UT == 32 ? lo : 0;
+  const uint16_t* src = p.rows[which] + layer * p.rows_layer_stride;
+
+  const unsigned n_new = !err && hi > lo ? hi - lo : 0;       // row r of the block is new iff r - lo < n_new
+  uint4 x[PASSES];
+  if (p.path_nodes) {
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      const int r = base + i * RPP + r_in;
+      x[i] = make_uint4(0, 0, 0, 0);
+      if ((unsigned)(r - lo) < n_new) {
+        const long long row = o + s_path[slot][(int)(t0 - start) + r];
+        if (SB_CHECKED_ACCESS(row, p.total_rows, &p.status[b]))
+          x[i] = __ldcs(reinterpret_cast<const uint4*>(src + row * p.row_stride + (long long)g * D + col));
       }
     }
+  } else {
+    const long long row_a = o + (t0 - start) + base + r_in;
+    const uint16_t* from = src + row_a * p.row_stride + (long long)g * D + col;
+    const long long pass = RPP * p.row_stride;
+#pragma unroll
+    for (int i = 0; i < PASSES; ++i) {
+      x[i] = make_uint4(0, 0, 0, 0);
+      if ((unsigned)(base + i * RPP + r_in - lo) < n_new && SB_CHECKED_ACCESS(row_a + i * RPP, p.total_rows, &p.status[b]))
+        x[i] = __ldcs(reinterpret_cast<const uint4*>(from + i * pass));
+    }
   }
-  __syncthreads();
-  err = s_err;
-  if (blockIdx.x == 0 && blockIdx.y == 0 && layer == 0 && tid == 0) {
+  if (!err && p.kv.page_size > 0 && n > 0) {
+    const int shift = 31 - __clz(p.kv.page_size);
+    bool bad = false;
+    for (int lp = (start >> shift) + tid; lp <= (start + n - 1) >> shift; lp += UT) {
+      const int page = p.kv.page_table[(long long)b * p.kv.max_pages + lp];
+      bad |= page < 0 || page >= p.kv.num_pages;
+    }
+    if (any(bad)) err = SB_ERR_BOUNDS;
+  }
+  if (first_unit && tid == 0) {
     p.status[b] = err;
     p.new_len[b] = err ? start : start + n;
   }
-  if (err || n == 0) return;
-  const int block = start / sb + blockIdx.x;                 // block of tokens of this sequence
-  const long long t0 = (long long)block * sb;
-  if (t0 >= (long long)start + n) return;
-  const int lo = (int)(t0 > start ? t0 : start) - (int)t0;    // new rows of the block: [lo, hi)
-  const int hi = (int)min((long long)start + n - t0, (long long)sb);
+  if (err || !mine || hi <= lo) return;
 
   const long long row0 = quant_row(p.kv, b, (int)t0);         // the block lies inside one page
   uint8_t* codes = static_cast<uint8_t*>(which ? p.kv.v_codes : p.kv.k_codes) + layer * p.kv.codes_layer_stride;
-  float* scale = (which ? p.kv.v_scale : p.kv.k_scale) + layer * p.kv.scale_layer_stride + (row0 / sb) * H + g;
-  const uint16_t* src = p.rows[which] + layer * p.rows_layer_stride;
-  const int r_in = tid / LPR, col = (tid % LPR) * 8;
-
-  uint4 x[PASSES];
-  uint32_t amax = 0;  // magnitudes order like integers; a NaN or an infinity is >= 0x7F80
+  float* scale = (which ? p.kv.v_scale : p.kv.k_scale) + layer * p.kv.scale_layer_stride + (row0 >> p.block_shift) * H + g;
+  const float old = lo > 0 ? *scale : 0.f;                    // older tokens share the block
+  // magnitudes order like integers; a NaN or an infinity is >= 0x7F80
+  auto unit_max = [&]() {
+    uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < PASSES; ++i) {
-    const int r = i * RPP + r_in;
-    x[i] = make_uint4(0, 0, 0, 0);
-    if (r >= lo && r < hi) {
-      const int j = (int)(t0 + r - start);
-      const long long row = o + (p.path_nodes ? s_path[j] : j);
-      if (SB_CHECKED_ACCESS(row, p.total_rows, &p.status[b]))
-        x[i] = *reinterpret_cast<const uint4*>(src + row * p.row_stride + (long long)g * D + col);
+    for (int i = 0; i < PASSES; ++i) {
       const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        amax = max(amax, w[k] & 0x7FFFu);
-        amax = max(amax, (w[k] >> 16) & 0x7FFFu);
-      }
+      for (int k = 0; k < 4; ++k) m = __vmaxu2(m, w[k] & 0x7FFF7FFFu);  // both halves at once
     }
-  }
-  amax = __reduce_max_sync(0xffffffffu, amax);
-  if ((tid & 31) == 0) s_max[tid >> 5] = amax;
-  __syncthreads();
+    m = __reduce_max_sync(0xffffffffu, max(m & 0xFFFFu, m >> 16));
+    if (UT > 32) {
+      __syncthreads();
+      if ((tid & 31) == 0) s_max[tid >> 5] = m;
+      __syncthreads();
 #pragma unroll
-  for (int i = 0; i < AP_THREADS / 32; ++i) amax = max(amax, s_max[i]);
+      for (int i = 0; i < UT / 32; ++i) m = max(m, s_max[i]);
+    }
+    return m;
+  };
+  uint32_t amax = unit_max();
   const bool bad = amax >= 0x7F80u;
   if (bad) {  // rare: the finite elements still get a scale of their own
-    uint32_t fin = 0;
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
       uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
@@ -131,58 +192,34 @@ __global__ void __launch_bounds__(AP_THREADS) kv_append_quant_kernel(const Appen
       for (int k = 0; k < 4; ++k) {
         if ((w[k] & 0x7F80u) == 0x7F80u) w[k] &= 0xFFFF0000u;
         if ((w[k] & 0x7F800000u) == 0x7F800000u) w[k] &= 0xFFFFu;
-        fin = max(fin, max(w[k] & 0x7FFFu, (w[k] >> 16) & 0x7FFFu));
       }
       x[i] = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    fin = __reduce_max_sync(0xffffffffu, fin);
-    __syncthreads();
-    if ((tid & 31) == 0) s_max[tid >> 5] = fin;
-    __syncthreads();
-    amax = 0;
-#pragma unroll
-    for (int i = 0; i < AP_THREADS / 32; ++i) amax = max(amax, s_max[i]);
+    amax = unit_max();
   }
   float s = __uint_as_float((uint32_t)(scale_exponent(amax << 16) + 127) << 23);
-  const float old = lo > 0 ? *scale : 0.f;  // older tokens share the block
   const bool was_bad = old != old;
   if (!was_bad && old > s) s = old;
-  __syncthreads();                          // every thread has read the old scale
+  sync();                                   // every thread has read the old scale
   if (tid == 0) *scale = (bad || was_bad) ? __uint_as_float(0x7FC00000u) : s;
   // Powers of two divide exactly by their reciprocal; an older scale of another writer may be any number.
   const float inv = 1.f / s;
-  const bool exact_inv = (__float_as_uint(s) & 0x7FFFFFu) == 0;
-  const bool grow = lo > 0 && !was_bad && old != s;
+  const bool exact = (__float_as_uint(s) & 0x7FFFFFu) == 0;
+  uint8_t* dst = codes + ((row0 + base + r_in) * H + g) * (long long)D + col;
+  const long long pass_bytes = (long long)RPP * H * D;
 #pragma unroll
   for (int i = 0; i < PASSES; ++i) {
-    const int r = i * RPP + r_in;
-    if (r >= hi) break;
-    const long long off = ((row0 + r) * H + g) * (long long)D + col;
-    if (!SB_CHECKED_ACCESS(off + 7, quant_rows_total(p.kv) * H * D, &p.status[b])) continue;
-    if (r >= lo) {
-      const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-      uint16_t c[4];
-#pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        const float a0 = __uint_as_float(w[k] << 16), a1 = __uint_as_float(w[k] & 0xFFFF0000u);
-        c[k] = exact_inv ? e4m3x2_of(a0 * inv, a1 * inv) : e4m3x2_of(a0 / s, a1 / s);
-      }
-      *reinterpret_cast<uint2*>(codes + off) = make_uint2(c[0] | ((uint32_t)c[1] << 16), c[2] | ((uint32_t)c[3] << 16));
-    } else if (grow) {
-      const uint2 was = *reinterpret_cast<const uint2*>(codes + off);
-      const uint32_t w[2] = {was.x, was.y};
-      uint32_t out[2];
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        uint16_t c[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float2 v = float2_of_e4m3x2((uint16_t)(w[k] >> (16 * e)));
-          c[e] = e4m3x2_of(v.x * old / s, v.y * old / s);
-        }
-        out[k] = c[0] | ((uint32_t)c[1] << 16);
-      }
-      *reinterpret_cast<uint2*>(codes + off) = make_uint2(out[0], out[1]);
+    const int r = base + i * RPP + r_in;
+    if ((unsigned)(r - lo) < n_new && SB_CHECKED_ACCESS(((row0 + r) * H + g) * D + col + 7, quant_rows_total(p.kv) * H * D, &p.status[b]))
+      *reinterpret_cast<uint2*>(dst + i * pass_bytes) = exact ? codes_times(x[i], inv) : codes_over(x[i], s);
+  }
+  if (lo > 0 && !was_bad && old != s) {     // the scale grew: the older codes follow
+#pragma unroll 4
+    for (int r = r_in; r < lo; r += RPP) {
+      const long long off = ((row0 + r) * H + g) * (long long)D + col;
+      if (!SB_CHECKED_ACCESS(off + 7, quant_rows_total(p.kv) * H * D, &p.status[b])) continue;
+      uint2* at = reinterpret_cast<uint2*>(codes + off);
+      *at = rescaled(*at, old, s);
     }
   }
 }
@@ -218,15 +255,23 @@ extern "C" sb_status sb_kv_append_quant(const sb_quant_cache* kv, const void* k_
   p.accept_len = accept_len;
   p.max_depth = max_depth;
   p.max_rows = max_rows;
+  p.block_shift = 31 - __builtin_clz((unsigned)kv->scale_block);
   p.len = len;
   p.new_len = new_len;
   p.status = status;
-  const long long zs = (long long)kv->batch * kv->n_layers, ys = 2LL * kv->n_kv_heads;
-  if (zs > 65535 || ys > 65535) return SB_ERR_UNSUPPORTED;
+  if (kv->n_layers > 65535 || kv->batch > 65535) return SB_ERR_UNSUPPORTED;
   const int most = path_nodes && max_depth + 1 < max_rows ? max_depth + 1 : max_rows;
+  const int sb = kv->scale_block;
   // blocks that `most` rows can touch, whatever the offset of the first
-  const dim3 grid(((unsigned)most + kv->scale_block - 2) / kv->scale_block + 1, (unsigned)ys, (unsigned)zs);
+  const long long units = (((long long)most + sb - 2) / sb + 1) * 2 * kv->n_kv_heads;
+  if (units > 0x7fffffffLL) return SB_ERR_UNSUPPORTED;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  return kv->head_dim == 64 ? launch_dependent(kv_append_quant_kernel<64>, grid, dim3(AP_THREADS), cs, p)
-                            : launch_dependent(kv_append_quant_kernel<128>, grid, dim3(AP_THREADS), cs, p);
+  auto launch = [&](auto kernel, int threads, int units_per_cta) {
+    return launch_dependent(kernel, dim3((unsigned)((units + units_per_cta - 1) / units_per_cta), kv->batch, kv->n_layers), dim3(threads), cs, p);
+  };
+  const bool d64 = kv->head_dim == 64;
+  if (most <= 16 || sb == 16) return d64 ? launch(kv_append_quant_kernel<64, 32>, 256, 8) : launch(kv_append_quant_kernel<128, 32>, 256, 8);
+  if (sb == 32) return d64 ? launch(kv_append_quant_kernel<64, 64>, 64, 1) : launch(kv_append_quant_kernel<128, 64>, 64, 1);
+  if (sb == 64) return d64 ? launch(kv_append_quant_kernel<64, 128>, 128, 1) : launch(kv_append_quant_kernel<128, 128>, 128, 1);
+  return d64 ? launch(kv_append_quant_kernel<64, 256>, 256, 1) : launch(kv_append_quant_kernel<128, 256>, 256, 1);
 }
