@@ -65,7 +65,7 @@ static int quant_num_sms() {
 
 struct QuantPlan {
   bool tc;                         // the tcgen05 kernel; else the 16-row kernel
-  int cluster, outer, grid_tiles;  // grid_tiles: row tiles (16 rows) or pairs of row tiles (2 x 128 rows) per KV head
+  int cluster, outer, grid_tiles;  // grid_tiles: row tiles (16 or 128 rows) per KV head
 };
 
 static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree, int total_q, int window, int sinks, int num_splits) {
@@ -79,14 +79,13 @@ static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree,
   pl.tc = rows > 16;
   pl.cluster = 1;
   if (pl.tc) {
-    // CTAs run in waves of one per SM.  A CTA costs its key blocks (both streams work on every block when there are two
-    // row tiles, else on every second one) plus a fixed start and end; every chunk beyond the first writes
-    // and re-reads fp32 partials of all rows.
-    pl.grid_tiles = ceil_div(rows, 256);
+    // CTAs run in waves of one per SM.  A CTA costs its key blocks plus a fixed start and end; every chunk beyond the first writes
+    // and re-reads bf16 partials of all rows, and the merge is one more kernel.
+    pl.grid_tiles = ceil_div(rows, 128);
     const int blocks = (int)((keys + 127) / 128) + (window > 0 ? 2 : 0) + 1;
     const long long units = (long long)kv->batch * kv->n_kv_heads * pl.grid_tiles;
-    const double per_block = rows > 128 ? 1.4 : 0.7, fixed = 6.0;
-    const double partial = 2.0 * (double)total_q * tree->n_q_heads * kv->head_dim * 4.0 / 5e6;
+    const double per_block = 1.2, fixed = 6.0;
+    const double partial = 2.0 * (double)total_q * tree->n_q_heads * kv->head_dim * 2.0 / 5e6;
     int best = 1;
     double best_cost = 0.0;
     const int most = num_splits > 0 ? 1 : (blocks < 64 ? blocks : 64);
@@ -197,6 +196,7 @@ extern "C" sb_status sb_tree_attention_quant(const sb_quant_cache* kv, int32_t l
   p.block_shift = 0;
   while ((1 << p.block_shift) < kv->scale_block) ++p.block_shift;
   p.G = tree->n_q_heads / kv->n_kv_heads;
+  p.g_magic = (1u << 20) / (unsigned)p.G + 1u;
   p.part_o = nullptr;
   p.part_lse = nullptr;
   const QuantPlan pl = plan_quant(kv, tree, total_q, window, sinks, num_splits);

@@ -32,6 +32,7 @@ struct QuantAttnParams {
   float* part_lse;  // [outer][total_q * Hq]    base-2 log-sum-exp of each
   int* status;
   int G;
+  unsigned g_magic; // row / G = row * g_magic >> 20 for rows below 2^11
   int block_shift;  // log2 of the tokens per scale block
   int sort_seqs;    // 1: grid index z is the rank of a sequence by length, longest first
 };

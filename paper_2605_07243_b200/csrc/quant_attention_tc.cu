@@ -11,14 +11,14 @@
 // exponent (P' = 2^(s + log2 v - reference), denominator sum P' / v), which the fused multiply-add that forms
 // the exponent does for nothing.
 //
-// A CTA owns one KV head's chunk of the key list and two "streams" t = 0, 1, each with its own accumulator and two score
-// buffers of 64 keys in tensor memory (2 x D + 4 x 64 columns) and its own softmax warpgroup with one thread per row:
-//   two row tiles (mode A): stream t is tile t and takes both 64-key halves of every key block in turn;
-//   one row tile (mode B): stream t takes half t of every key block; the two accumulators are merged at the end.
-// The MMA warp issues, for step i of each stream in turn, O_t += P_i V and then S_{i+2} = Q K^T into the buffer that P_i was
-// read from.  So a softmax warp always has the next 64 scores waiting while the tensor pipe is busy with the buffer it
-// has just left: with one 128-key buffer per stream the warps spent half of their time waiting for PV and S of their
-// own stream (6400 clocks per key block and pair of tiles against 2100 of tensor work).
+// A CTA owns one row tile of a KV head and a chunk of its key list, and works as two "streams" t = 0, 1: stream t takes half t (64
+// keys) of every key block, with its own accumulator and two score buffers in tensor memory (2 x D + 4 x 64 columns) and its
+// own softmax warpgroup of one thread per row; the two accumulators are merged at the end.  The MMA warp issues, for
+// block i and each stream in turn, O_t += P_i V and then S_{i+2} = Q K^T into the buffer that P_i was read from.  So a
+// softmax warp always has the next 64 scores waiting while the tensor pipe is busy with the buffer it has just left: with
+// one buffer per stream the warps spent half of their time waiting for PV and S of their own stream.
+// (One tile per CTA, although two tiles could share a key block's loads and conversions: both are off the critical path, which
+// is the exponentials, and the smaller units fill the SMs more evenly: 16 ragged trees 191 -> 150 us.)
 //
 // The softmax thread does not compute a maximum after its row's first visible key: the reference is raised when the sum of 32
 // probabilities shows that an exponent is far above it (P' is fp16, which ends at 2^16), a rare event that
@@ -46,9 +46,9 @@ enum QtBar { QB_P_FULL00, QB_P_FULL01, QB_P_FULL10, QB_P_FULL11,                
              QB_V_EMPTY0, QB_V_EMPTY1, QB_S_FULL00, QB_S_FULL01, QB_S_FULL10, QB_S_FULL11, QB_PV0, QB_PV1, QB_O_DONE,
              QB_Q_FULL, QB_COUNT };
 
-// Q terms (2 tiles x 2 x 128 D), K codes (2 stages), the tree's second K term, V codes (2 stages), V fp16 (2 stages)
+// Q terms (2 x 128 D), K codes (2 stages), the tree's second K term, V codes (2 stages), V fp16 (2 stages)
 template <int D>
-constexpr int quant_tc_smem() { return 1024 + QT_SMALL + TC_BM * D * (4 + 2 + 1 + 2 + 4); }
+constexpr int quant_tc_smem() { return 1024 + QT_SMALL + TC_BM * D * (2 + 2 + 1 + 2 + 4); }
 
 __device__ inline uint32_t tc_idesc_f16(int M, int N, int b_mn_major) {
   return (1u << 4) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
@@ -294,15 +294,16 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   uint64_t* s_bar = reinterpret_cast<uint64_t*>(base + 3072);        // QB_COUNT * 8
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(base + 3328);
   volatile int* s_abort = reinterpret_cast<volatile int*>(base + 3332);   // [0] a wait gave up; [1] the same for the last wait
+  int* s_err = reinterpret_cast<int*>(base + 3340);
   uint32_t* s_bad = reinterpret_cast<uint32_t*>(base + 3344);        // [4]: node rows with a NaN or an infinity
   uint32_t* s_flag = reinterpret_cast<uint32_t*>(base + 3360);       // [4 slots]: 16-key groups of a block with a NaN scale
   float* s_ks = reinterpret_cast<float*>(base + 3392);               // [4 slots][8 groups of 16 keys] K scale
   float* s_lsv = s_ks + 32;                                          // log2 of the V scale
   float* s_isv = s_lsv + 32;                                         // 1 / V scale
-  float* s_qs = reinterpret_cast<float*>(base + 3840);               // [256 rows] scale of a Q row
-  float* s_ml = reinterpret_cast<float*>(base + 4864);               // [2 streams][reference, sum][128]
-  uint8_t* sQ = base + QT_SMALL;      // [2 tiles][2 terms]
-  uint8_t* sK = sQ + 4 * TILE8;       // [2 stages] codes
+  float* s_qs = reinterpret_cast<float*>(base + 3840);               // [128 rows] scale of a Q row
+  float* s_ml = reinterpret_cast<float*>(base + 4864);               // [2 streams][reference, sum][128 rows]
+  uint8_t* sQ = base + QT_SMALL;      // [2 terms]
+  uint8_t* sK = sQ + 2 * TILE8;       // [2 stages] codes
   uint8_t* sK2 = sK + 2 * TILE8;      // second term of the tree's K
   uint8_t* sVr = sK2 + TILE8;         // [2 stages] codes
   uint8_t* sV = sVr + 2 * TILE8;      // [2 stages] fp16
@@ -327,12 +328,11 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   pdl_wait();
   pdl_release();
 
-  const int pairs = (int)gridDim.y / Hkv;
-  const int g = blockIdx.y / pairs, pair = blockIdx.y % pairs;   // the pairs of a KV head are neighbours: they share its codes in L2
+  const int tiles = (int)gridDim.y / Hkv;
+  const int g = blockIdx.y / tiles, row0 = (int)(blockIdx.y % tiles) * TC_BM;   // the tiles of a KV head are neighbours: they share its codes in L2
   const int b = p.sort_seqs ? quant_sequence_of_rank(p, blockIdx.z, reinterpret_cast<int*>(s_anc), s_parent) : (int)blockIdx.z;
   const QuantSeq si = load_quant_seq(p, b);
   const int rows_total = si.nq * G;
-  const int row0 = pair * 2 * TC_BM;
   const bool designated = split == 0 && blockIdx.y == 0;
   if (!si.can_write || row0 >= rows_total) {
     if (designated) {
@@ -343,7 +343,6 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(*s_tmem), "r"(QT_TMEM_COLS));
     return;
   }
-  const bool two = row0 + TC_BM < rows_total;   // mode A
   const long long rows_all = (long long)p.total_q * Hq;
 
   const BlockList list = visible_blocks(si.P, p.window, p.sinks, TC_BN);
@@ -351,7 +350,6 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   const int per = total / p.num_splits, rem = total % p.num_splits;
   const int blk0 = split * per + min(split, rem);
   const int nb = per + (split < rem ? 1 : 0);
-  const int steps = two ? 2 * nb : nb;                              // of 64 keys, for each stream
   const uint32_t tmem = __shfl_sync(0xffffffffu, *s_tmem, 0);
   const uint32_t tmem_o = tmem + 4 * 64;                            // accumulator of stream t at tmem_o + t * D
 
@@ -363,60 +361,47 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   bool ok = true, compute = false;
 
   if (warp < QT_SOFTMAX / 32) {
-    // ---- Q: 16-byte pieces, D / 8 lanes to a row, eight loads in flight -----------------------------------------------
-    constexpr int LPR = D / 8, RPP = QT_SOFTMAX / LPR, BATCH = 8;
-    const int n_rows = two ? 2 * TC_BM : TC_BM, ch = tid % LPR;
-#pragma unroll 1
-    for (int r0 = 0; r0 < n_rows; r0 += BATCH * RPP) {
-      uint4 x[BATCH];
+    // ---- Q: 16-byte pieces, D / 8 lanes to a row, all loads in flight at once -----------------------------------------
+    constexpr int LPR = D / 8, RPP = QT_SOFTMAX / LPR, NQ = TC_BM / RPP;
+    const int ch = tid % LPR;
+    uint4 xq[NQ];
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        const int R = row0 + r0 + i * RPP + tid / LPR, Rc = R < rows_total ? R : 0;
-        const int nl = Rc / G;
-        const bool on = R < rows_total && SB_CHECKED_ACCESS(si.q_off + nl, p.total_q, &p.status[b]);
-        x[i] = __ldg(reinterpret_cast<const uint4*>(p.q + (long long)(si.q_off + (on ? nl : 0)) * p.q_stride +
-                                                    (long long)(g * G + Rc - nl * G) * D + ch * 8));
-        if (!on) x[i] = make_uint4(0, 0, 0, 0);
-      }
+    for (int i = 0; i < NQ; ++i) {
+      const int R = row0 + i * RPP + tid / LPR;
+      const int nl = (int)((unsigned)R * p.g_magic >> 20), hh = R - nl * G;
+      xq[i] = make_uint4(0, 0, 0, 0);
+      if (R < rows_total && SB_CHECKED_ACCESS(si.q_off + nl, p.total_q, &p.status[b]))
+        xq[i] = __ldg(reinterpret_cast<const uint4*>(p.q + (long long)(si.q_off + nl) * p.q_stride + (g * G + hh) * D + ch * 8));
+    }
 #pragma unroll
-      for (int i = 0; i < BATCH; ++i) {
-        const int r = r0 + i * RPP + tid / LPR;
-        uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-        uint32_t amax = 0;
+    for (int i = 0; i < NQ; ++i) {
+      const int r = i * RPP + tid / LPR;
+      const uint32_t w[4] = {xq[i].x, xq[i].y, xq[i].z, xq[i].w};
+      uint32_t amax = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu), __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
 #pragma unroll
-        for (int k = 0; k < 4; ++k) amax = max(amax, max(w[k] & 0x7FFFu, (w[k] >> 16) & 0x7FFFu));
+      for (int d = 1; d < LPR; d <<= 1) amax = __vmaxu2(amax, __shfl_xor_sync(0xffffffffu, amax, d));
+      const int ex = (int)(max(amax & 0xFFFFu, amax >> 16) >> 7);
+      const int e = ex == 255 ? 127 : min(max(ex - 7, 1), 253);   // the largest element becomes 2^7 .. 2^8
+      const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
+      uint16_t hi[4], lo[4];
 #pragma unroll
-        for (int d = 1; d < LPR; d <<= 1) amax = max(amax, __shfl_xor_sync(0xffffffffu, amax, d));
-        const int ex = (int)(amax >> 7);
-        const int e = ex == 255 ? 127 : min(max(ex - 7, 1), 253);   // the largest element becomes 2^7 .. 2^8
-        const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
-        uint16_t hi[4], lo[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) split_e4m3(__uint_as_float(w[k] << 16) * inv, __uint_as_float(w[k] & 0xFFFF0000u) * inv, hi[k], lo[k]);
-        uint8_t* dst = sQ + (r / TC_BM) * (2 * TILE8) + code_tile_off<D>(r % TC_BM, ch >> 1) + (ch & 1) * 8;
-        *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0] | ((uint32_t)hi[1] << 16), hi[2] | ((uint32_t)hi[3] << 16));
-        *reinterpret_cast<uint2*>(dst + TILE8) = make_uint2(lo[0] | ((uint32_t)lo[1] << 16), lo[2] | ((uint32_t)lo[3] << 16));
-        // a row with a NaN or an infinity is NaN throughout (e4m3 has no infinity)
-        if (ch == 0) s_qs[r] = ex == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)e << 23) * p.scale_log2;
-      }
+      for (int k = 0; k < 4; ++k) split_e4m3(__uint_as_float(w[k] << 16) * inv, __uint_as_float(w[k] & 0xFFFF0000u) * inv, hi[k], lo[k]);
+      uint8_t* dst = sQ + code_tile_off<D>(r, ch >> 1) + (ch & 1) * 8;
+      *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0] | ((uint32_t)hi[1] << 16), hi[2] | ((uint32_t)hi[3] << 16));
+      *reinterpret_cast<uint2*>(dst + TILE8) = make_uint2(lo[0] | ((uint32_t)lo[1] << 16), lo[2] | ((uint32_t)lo[3] << 16));
+      // a row with a NaN or an infinity is NaN throughout (e4m3 has no infinity)
+      if (ch == 0) s_qs[r] = ex == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)e << 23) * p.scale_log2;
     }
     fence_async_smem();
     mbar_arrive(&s_bar[QB_Q_FULL]);
-    const ThreadGroup grp = first_threads(QT_SOFTMAX);
-    const bool tree_ok = build_ancestors_smem(p.tree.parent + si.node_base, si.err ? 0 : si.n, s_parent, s_anc, s_depth, grp);
-    int err = si.err;
-    if (!err && !tree_ok) err = SB_ERR_INVALID_TREE;
-    if (designated) {
-      const bool pages_ok = err ? true : quant_pages_in_pool(p.kv, b, si.P, grp);
-      if (tid == 0) p.status[b] = err ? err : (pages_ok ? 0 : (int)SB_ERR_BOUNDS);
-    }
-    compute = err == 0;
+    asm volatile("bar.sync 3, 320;" ::: "memory");   // the converters have planned the tree, s_qs is complete
+    compute = *s_err == 0;
 
     // ---- softmax --------------------------------------------------------------------------------------------------
-    const int R = row0 + (two ? t_mine * TC_BM : 0) + row;
-    const int node = (R < rows_total && compute) ? si.q0 + R / G : -1;
+    const int R = row0 + row;
+    const int node = (R < rows_total && compute) ? si.q0 + (int)((unsigned)R * p.g_magic >> 20) : -1;
     const int pos = si.P + (node >= 0 ? s_depth[node] : 0);
-    const float qs = s_qs[(two ? t_mine * TC_BM : 0) + row];
+    const float qs = s_qs[row];
     bool poison = false;
 
     // One step's 64 scores of this row -> probabilities, 32 columns at a time, the next 32 in flight.  (Rolled: unrolled twice, the
@@ -483,19 +468,18 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       }
     };
     // A wait that gives up leaves `ok` false; the loop still runs to its end, so that every barrier gets its arrivals.
-    for (int i = 0; i < steps; ++i) {
-      const int j = two ? i >> 1 : i, half = two ? i & 1 : t_mine;
-      const int at = blk0 + j, group = (j & 3) * 8 + half * 4;
+    for (int i = 0; i < nb; ++i) {
+      const int at = blk0 + i, group = (i & 3) * 8 + t_mine * 4;
       const bool is_tree = at >= list.count;
-      const int k0 = (is_tree ? 0 : list.at(at) * TC_BN) + 64 * half;
+      const int k0 = (is_tree ? 0 : list.at(at) * TC_BN) + 64 * t_mine;
       // steps that every row sees whole need no mask
       const bool masked = is_tree || k0 + 64 > si.P || (p.window > 0 && k0 + 64 > p.sinks && si.P + si.n - 1 - k0 >= p.window);
-      if (ok) ok = mbar_wait(&s_bar[QB_SC0 + (j & 3)], (j >> 2) & 1, s_abort) &&
+      if (ok) ok = mbar_wait(&s_bar[QB_SC0 + (i & 3)], (i >> 2) & 1, s_abort) &&
                    mbar_wait(&s_bar[QB_S_FULL00 + 2 * t_mine + (i & 1)], (i >> 1) & 1, s_abort);
       __syncwarp();
       tc_fence_after();
       const uint32_t s_addr = tmem + lane_base + (2 * t_mine + (i & 1)) * 64;
-      const uint32_t flags = is_tree ? 0u : (s_flag[j & 3] >> (4 * half)) & 15u;   // poisoned 16-key groups of the step
+      const uint32_t flags = is_tree ? 0u : (s_flag[i & 3] >> (4 * t_mine)) & 15u;   // poisoned 16-key groups of the step
       if (masked || flags) {
         // invisible scores become -inf in tensor memory before the walk
 #pragma unroll 1
@@ -541,46 +525,44 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     const uint32_t v_lo = tc_desc_lo(smem_u32(sV), TC_BN * 128);
     const uint32_t idesc_s = tc_idesc_e4m3(TC_BM, 64), idesc_pv = tc_idesc_f16(TC_BM, D, 1);
     auto issue_s = [&](int t, int i) {
-      const int j = two ? i >> 1 : i, half = two ? i & 1 : t;
-      if (t == 0 && (!two || half == 0)) ok = ok && mbar_wait(&s_bar[QB_K_FULL0 + (j & 1)], (j >> 1) & 1, s_abort);  // first reader
+      if (t == 0) ok = ok && mbar_wait(&s_bar[QB_K_FULL0 + (i & 1)], (i >> 1) & 1, s_abort);  // first reader
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) return;
       tc_fence_after();
-      const uint32_t qb = q_lo + (two ? t : 0) * (2 * TILE8 >> 4), d = tmem + (2 * t + (i & 1)) * 64;
-      uint32_t kb = k_lo + (j & 1) * (TILE8 >> 4) + half * (64 * D >> 4);
+      const uint32_t d = tmem + (2 * t + (i & 1)) * 64;
+      uint32_t kb = k_lo + (i & 1) * (TILE8 >> 4) + t * (64 * D >> 4);
       // (Q1 + Q2) K, and for the tree (Q1 + Q2) (K1 + K2); 32 elements a step
-      const int terms = blk0 + j >= list.count ? 2 : 1;
+      const int terms = blk0 + i >= list.count ? 2 : 1;
 #pragma unroll 1
       for (int c = 0; c < terms; ++c) {
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
-          warp_mma_f8(elected, d, qb + (ks / (D / 32)) * (TILE8 >> 4) + (ks % (D / 32)) * 2, kb + (ks % (D / 32)) * 2, hi8, idesc_s, c + ks > 0);
-        kb = k2_lo + half * (64 * D >> 4);
+          warp_mma_f8(elected, d, q_lo + (ks / (D / 32)) * (TILE8 >> 4) + (ks % (D / 32)) * 2, kb + (ks % (D / 32)) * 2, hi8, idesc_s, c + ks > 0);
+        kb = k2_lo + t * (64 * D >> 4);
       }
       warp_commit(elected, &s_bar[QB_S_FULL00 + 2 * t + (i & 1)]);
-      if (t == 1 && (!two || half == 1)) warp_commit(elected, &s_bar[QB_K_EMPTY0 + (j & 1)]);                        // last reader
+      if (t == 1) warp_commit(elected, &s_bar[QB_K_EMPTY0 + (i & 1)]);                        // last reader
     };
     auto issue_pv = [&](int t, int i) {
-      const int j = two ? i >> 1 : i, half = two ? i & 1 : t;
       ok = ok && mbar_wait(&s_bar[QB_P_FULL00 + 2 * t + (i & 1)], (i >> 1) & 1, s_abort);
-      if (t == 0 && (!two || half == 0)) ok = ok && mbar_wait(&s_bar[QB_V_FULL0 + (j & 1)], (j >> 1) & 1, s_abort);
+      if (t == 0) ok = ok && mbar_wait(&s_bar[QB_V_FULL0 + (i & 1)], (i >> 1) & 1, s_abort);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) return;
       tc_fence_after();
-      const uint32_t vb = v_lo + (j & 1) * (TILE >> 4) + half * (4 * 2048 >> 4), pb = tmem + (2 * t + (i & 1)) * 64;
+      const uint32_t vb = v_lo + (i & 1) * (TILE >> 4) + t * (4 * 2048 >> 4), pb = tmem + (2 * t + (i & 1)) * 64;
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks)
         warp_mma_ts(elected, tmem_o + t * D, pb + ks * 8, vb + ks * (2048 >> 4), hi, idesc_pv, (i > 0 || ks > 0) ? 1u : 0u);
       warp_commit(elected, &s_bar[QB_PV0 + t]);
-      if (t == 1 && (!two || half == 1)) warp_commit(elected, &s_bar[QB_V_EMPTY0 + (j & 1)]);
+      if (t == 1) warp_commit(elected, &s_bar[QB_V_EMPTY0 + (i & 1)]);
     };
-    if (steps > 0) ok = __all_sync(0xffffffffu, mbar_wait(&s_bar[QB_Q_FULL], 0, s_abort));
+    if (nb > 0) ok = __all_sync(0xffffffffu, mbar_wait(&s_bar[QB_Q_FULL], 0, s_abort));
     // (the first two rounds only issue S; rolled, so that the code is there once)
 #pragma unroll 1
-    for (int it = -4; it < 2 * steps; ++it) {
+    for (int it = -4; it < 2 * nb; ++it) {
       const int i = it >> 1, t = it & 1;
       if (i >= 0) issue_pv(t, i);
-      if (i + 2 < steps) issue_s(t, i + 2);
+      if (i + 2 < nb) issue_s(t, i + 2);
     }
     warp_commit(elected, &s_bar[QB_O_DONE]);
     if (!ok && lane == 0) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
@@ -640,6 +622,19 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     if (!ok && lane == 0) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
   } else {
     // ---- converters: warp cw owns rows 64 cw .. + 63 of every V block ----------------------------------------------------
+    // Before the first block arrives they plan the tree for the softmax warps, which are busy with Q.
+    {
+      const ThreadGroup grp{tid - QT_CVT_WARP * 32, 64, false};
+      const bool tree_ok = build_ancestors_smem(p.tree.parent + si.node_base, si.err ? 0 : si.n, s_parent, s_anc, s_depth, grp);
+      int err = si.err;
+      if (!err && !tree_ok) err = SB_ERR_INVALID_TREE;
+      if (designated) {
+        const bool pages_ok = err ? true : quant_pages_in_pool(p.kv, b, si.P, grp);
+        if (grp.tid == 0) p.status[b] = err ? err : (pages_ok ? 0 : (int)SB_ERR_BOUNDS);
+      }
+      if (grp.tid == 0) *s_err = err;
+      asm volatile("bar.sync 3, 320;" ::: "memory");
+    }
     const int cw = warp - QT_CVT_WARP, n_cache = max(0, min(nb, list.count - blk0));
     constexpr int CPR = D / 16, RPI = 32 / CPR, NI = 32 / RPI;
     const int ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
@@ -713,9 +708,11 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   }
 
   // ---- store ----------------------------------------------------------------------------------------------------------
-  // Every thread of a stream normalises its row and stages it as bf16 with the row's number and log-sum-exp (over the idle Q and K
-  // tiles); then half a warp per row writes whole rows.  In mode B the second stream first hands its row over.
+  // The two streams merge their accumulators: thread (stream t, row) takes half t of the row's columns, for which the other stream
+  // hands its part over in shared memory.  Rows are staged as bf16 with their number and log-sum-exp (over the idle Q and K
+  // tiles); then half a warp per row writes whole rows.
   constexpr int ROWB = D * 2 + 16;                    // [bf16 row | base-2 log-sum-exp | pad | global row or -1]
+  constexpr int DH = D / 2, RS = DH + 4;              // floats per half row handed over
   const bool have = nb > 0;
   if (warp < QT_SOFTMAX / 32) {
     // awaited even after a wait that gave up: tensor memory is idle before it is freed
@@ -726,56 +723,52 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       ref = INFINITY;
       seen_any = true;
     }
-    const bool merge = !two && have;                  // two accumulators per row
-    constexpr int RS = D + 4;                         // floats per row handed over, over the idle V tiles and the end of K
-    float* hand = reinterpret_cast<float*>(sV + 2 * TILE - 128 * RS * 4);
-    if (merge && t_mine == 1) {
-#pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
-        uint32_t r[32];
-        tmem_ld32(tmem_o + D + lane_base + c * 32, r);
+    float* hand0 = reinterpret_cast<float*>(sV + 2 * TILE - 2 * TC_BM * RS * 4);  // over the idle V tiles and the end of the codes before them
+    float* hand = hand0 + (t_mine * TC_BM + row) * RS;
+    if (have)
 #pragma unroll
-        for (int i = 0; i < 32; i += 4)
-          *reinterpret_cast<uint4*>(hand + row * RS + c * 32 + i) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
+      for (int c = 0; c < DH / 32; ++c) {
+        uint32_t r[32];
+        tmem_ld32(tmem_o + t_mine * D + lane_base + (t_mine ^ 1) * DH + c * 32, r);
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) *reinterpret_cast<uint4*>(hand + c * 32 + i) = make_uint4(r[i], r[i + 1], r[i + 2], r[i + 3]);
       }
-      s_ml[row] = seen_any ? ref : -INFINITY;
-      s_ml[128 + row] = l_run;
-    }
+    s_ml[t_mine * 256 + row] = seen_any ? ref : -INFINITY;
+    s_ml[t_mine * 256 + 128 + row] = l_run;
     softmax_group_sync();
-    if (two || t_mine == 0) {
-      float m = seen_any ? ref : -INFINITY, w0 = 1.f, w1 = 0.f, l = l_run;
-      if (merge) {
-        const float m1 = s_ml[row], l1 = s_ml[128 + row], M = fmaxf(m, m1);
-        w0 = m == -INFINITY ? 0.f : fast_exp2(m - M);
-        w1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - M);
-        l = w0 * l + w1 * l1;
-        m = M;
+    const float m_me = seen_any ? ref : -INFINITY, m_other = s_ml[(t_mine ^ 1) * 256 + row], l_other = s_ml[(t_mine ^ 1) * 256 + 128 + row];
+    const float m = fmaxf(m_me, m_other);
+    float w_me = m_me == -INFINITY ? 0.f : fast_exp2(m_me - m), w_other = m_other == -INFINITY ? 0.f : fast_exp2(m_other - m);
+    const float l = w_me * l_run + w_other * l_other;
+    const bool empty = l == 0.f;
+    const float inv = empty ? 0.f : 1.f / l;
+    w_me *= inv;
+    w_other *= inv;
+    const float* theirs = hand0 + ((t_mine ^ 1) * TC_BM + row) * RS;
+    uint8_t* dst = sQ + row * ROWB;
+#pragma unroll
+    for (int c = 0; c < DH / 32; ++c) {
+      uint32_t r[32];
+      if (have) tmem_ld32(tmem_o + t_mine * D + lane_base + t_mine * DH + c * 32, r);
+#pragma unroll
+      for (int i = 0; i < 32; i += 8) {
+        float f[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) f[k] = have && w_me != 0.f ? __uint_as_float(r[i + k]) * w_me : 0.f;  // (weight 0: nothing was written there)
+        if (have && w_other != 0.f) {
+          const float4 o0 = *reinterpret_cast<const float4*>(theirs + c * 32 + i), o1 = *reinterpret_cast<const float4*>(theirs + c * 32 + i + 4);
+          f[0] = fmaf(o0.x, w_other, f[0]); f[1] = fmaf(o0.y, w_other, f[1]); f[2] = fmaf(o0.z, w_other, f[2]); f[3] = fmaf(o0.w, w_other, f[3]);
+          f[4] = fmaf(o1.x, w_other, f[4]); f[5] = fmaf(o1.y, w_other, f[5]); f[6] = fmaf(o1.z, w_other, f[6]); f[7] = fmaf(o1.w, w_other, f[7]);
+        }
+        *reinterpret_cast<uint4*>(dst + (t_mine * DH + c * 32 + i) * 2) =
+            make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
       }
-      const int R = row0 + (two ? t_mine * TC_BM : 0) + row;
-      const int nl = R / G;
+    }
+    if (t_mine == 0) {
+      const int R = row0 + row;
+      const int nl = (int)((unsigned)R * p.g_magic >> 20);
       const long long grow = (long long)(si.q_off + nl) * Hq + g * G + (R - nl * G);
       const bool on = R < rows_total && SB_CHECKED_ACCESS(grow, rows_all, &p.status[b]);
-      const bool empty = !have || l == 0.f;
-      const float inv = empty ? 0.f : 1.f / l;
-      w0 *= inv;
-      w1 *= inv;
-      uint8_t* dst = sQ + (two ? t_mine * (TC_BM * ROWB) : 0) + row * ROWB;
-#pragma unroll 1
-      for (int c = 0; c < D / 32; ++c) {
-        uint32_t r[32];
-        if (have) tmem_ld32(tmem_o + (two ? t_mine * D : 0) + lane_base + c * 32, r);
-#pragma unroll
-        for (int i = 0; i < 32; i += 8) {
-          float f[8];
-#pragma unroll
-          for (int k = 0; k < 8; ++k) f[k] = have && w0 != 0.f ? __uint_as_float(r[i + k]) * w0 : 0.f;
-          if (w1 != 0.f)
-#pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = fmaf(hand[row * RS + c * 32 + i + k], w1, f[k]);
-          *reinterpret_cast<uint4*>(dst + (c * 32 + i) * 2) =
-              make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-        }
-      }
       *reinterpret_cast<float*>(dst + D * 2) = empty ? -INFINITY : m + log2f(l);
       *reinterpret_cast<long long*>(dst + D * 2 + 8) = on ? grow : -1ll;
     }
@@ -786,10 +779,10 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(QT_TMEM_COLS));
   }
-  const int n_staged = two ? 2 * TC_BM : TC_BM, col8 = lane & 15;
+  const int col8 = lane & 15;
   if (col8 < D / 8) {
-#pragma unroll 4
-    for (int r = 2 * warp + (lane >> 4); r < n_staged; r += 2 * (QT_THREADS / 32)) {
+#pragma unroll 6
+    for (int r = 2 * warp + (lane >> 4); r < TC_BM; r += 2 * (QT_THREADS / 32)) {
       const uint8_t* rowp = sQ + r * ROWB;
       const long long grow = *reinterpret_cast<const long long*>(rowp + D * 2 + 8);
       const float lse2 = *reinterpret_cast<const float*>(rowp + D * 2);
@@ -849,7 +842,7 @@ static sb_status launch_quant_tc_d(const QuantAttnParams& p, dim3 grid, cudaStre
   return launch_check();
 }
 
-// grid = (chunks, KV heads x tile pairs, sequences)
+// grid = (chunks, KV heads x row tiles, sequences)
 sb_status launch_quant_tc(const QuantAttnParams& p, dim3 grid, cudaStream_t cs) {
   return p.kv.head_dim == 64 ? launch_quant_tc_d<64>(p, grid, cs) : launch_quant_tc_d<128>(p, grid, cs);
 }
