@@ -14,7 +14,7 @@
 // A CTA owns one row tile of a KV head and a chunk of its key list, and works as two "streams" t = 0, 1: stream t takes half t (64
 // keys) of every key block, with its own accumulator and two score buffers in tensor memory (2 x D + 4 x 64 columns) and its
 // own softmax warpgroup of one thread per row; the two accumulators are merged at the end.  The MMA warp issues, for
-// block i and each stream in turn, O_t += P_i V and then S_{i+2} = Q K^T into the buffer that P_i was read from.  So a
+// block i, O_t += P_i V of both streams and then S_{i+2} = Q K^T, 128 keys at once, into the buffers that P_i was read from.  So a
 // softmax warp always has the next 64 scores waiting while the tensor pipe is busy with the buffer it has just left: with
 // one buffer per stream the warps spent half of their time waiting for PV and S of their own stream.
 // (One tile per CTA, although two tiles could share a key block's loads and conversions: both are off the critical path, which
@@ -24,8 +24,9 @@
 // probabilities shows that an exponent is far above it (P' is fp16, which ends at 2^16), a rare event that
 // rescales the accumulator.
 //
-// Prefix blocks come from the window's block list (128 keys); the tree's nodes are one last block of their own, scaled by a
-// power of two per 16 rows as if they were codes: K as two e4m3 terms, V as fp16.
+// The tree's nodes are one block of their own, the first of the list: the softmax warps bring it into the first stages before anything
+// else, scaled by a power of two per 16 rows as if they were codes (K as two e4m3 terms, V as fp16).  Then come the prefix
+// blocks of 128 keys that the window leaves.
 #include "quant_attention.cuh"
 #include "tc_common.cuh"
 
@@ -34,7 +35,7 @@ namespace sb {
 constexpr int QT_SOFTMAX = 256;       // warps 0-3: stream 0, warps 4-7: stream 1
 constexpr int QT_MMA_WARP = 8;
 constexpr int QT_LOAD_WARP = 9;       // K and V tiles by TMA, scales
-constexpr int QT_CVT_WARP = 10;       // warps 10, 11: V codes -> fp16, and the tree block
+constexpr int QT_CVT_WARP = 10;       // warps 10, 11: V codes -> fp16
 constexpr int QT_THREADS = 384;       // 12 warps leave 168 registers a thread
 constexpr int QT_TMEM_COLS = 512;
 constexpr int QT_SMALL = 8192;
@@ -43,7 +44,7 @@ constexpr float kQuantLimit = 8192.f; // sum of 32 probabilities relative to the
 enum QtBar { QB_P_FULL00, QB_P_FULL01, QB_P_FULL10, QB_P_FULL11,                              // 128 arrivals: a stream's threads
              QB_V_FULL0, QB_V_FULL1, QB_VR_EMPTY0, QB_VR_EMPTY1,                              // 2: the converter warps
              QB_K_FULL0, QB_K_FULL1, QB_VR_FULL0, QB_VR_FULL1, QB_SC0, QB_SC1, QB_SC2, QB_SC3, QB_K_EMPTY0, QB_K_EMPTY1,
-             QB_V_EMPTY0, QB_V_EMPTY1, QB_S_FULL00, QB_S_FULL01, QB_S_FULL10, QB_S_FULL11, QB_PV0, QB_PV1, QB_O_DONE,
+             QB_V_EMPTY0, QB_V_EMPTY1, QB_S_FULL0, QB_S_FULL1, QB_PV0, QB_PV1, QB_O_DONE,
              QB_Q_FULL, QB_COUNT };
 
 // Q terms (2 x 128 D), K codes (2 stages), the tree's second K term, V codes (2 stages), V fp16 (2 stages)
@@ -173,13 +174,11 @@ __device__ inline int lane_chunk(int lane) { return D == 128 ? (lane & 3) | ((la
 template <int D>
 __device__ inline int lane_row(int lane) { return D == 128 ? ((lane >> 2) & 1) | ((lane >> 3) & 2) : lane >> 2; }
 
-// 16 node rows (from row 16 * grp of `src`, n of them exist): this lane's 16 elements of each of its rows.  Rows that hold a NaN
-// or an infinity become zeros; their bits are returned.
+// 16 node rows (from row 16 * grp of `src`, n of them exist): this lane's 16 elements of each of its rows.
 template <int D>
-__device__ inline uint32_t node_rows(const bf16* src, long long stride, int n, int grp, int lane, uint4 (&x)[D / 16]) {
+__device__ inline void load_node_rows(const bf16* src, long long stride, int n, int grp, int lane, uint4 (&x)[D / 16]) {
   constexpr int RPI = 512 / D, NI = 16 / RPI;
   const int ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
-  uint32_t bits = 0;
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const int nd = 16 * grp + i * RPI + r_in;
@@ -190,16 +189,26 @@ __device__ inline uint32_t node_rows(const bf16* src, long long stride, int n, i
       x[2 * i + 1] = s4[1];
     }
   }
+}
+// Rows that hold a NaN or an infinity become zeros; their bits (of 16) are returned.
+template <int D>
+__device__ inline uint32_t drop_bad_rows(int lane, uint4 (&x)[D / 16]) {
+  constexpr int RPI = 512 / D, NI = 16 / RPI;
+  const int r_in = lane_row<D>(lane);
+  uint32_t mine = 0;  // bit i: this lane's part of its i-th row
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     const uint32_t w[8] = {x[2 * i].x, x[2 * i].y, x[2 * i].z, x[2 * i].w, x[2 * i + 1].x, x[2 * i + 1].y, x[2 * i + 1].z, x[2 * i + 1].w};
     bool nf = false;
 #pragma unroll
     for (int k = 0; k < 8; ++k) nf |= bf16x2_nonfinite(w[k]);
-    const uint32_t mine = __reduce_or_sync(0xffffffffu, nf ? 1u << r_in : 0u);
-    if ((mine >> r_in) & 1u) x[2 * i] = x[2 * i + 1] = make_uint4(0, 0, 0, 0);
-    bits |= mine << (i * RPI);
+    if (nf) mine |= 1u << (i * RPI + r_in);
   }
+  const uint32_t bits = __reduce_or_sync(0xffffffffu, mine);
+  if (bits)
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      if ((bits >> (i * RPI + r_in)) & 1u) x[2 * i] = x[2 * i + 1] = make_uint4(0, 0, 0, 0);
   return bits;
 }
 // Biased exponent e of the power of two 2^(e - 127) that takes 16 rows to magnitudes below 2^(up + 1).
@@ -215,40 +224,37 @@ __device__ inline int node_exponent(const uint4 (&x)[N], int up, int least) {
   amax = __reduce_max_sync(0xffffffffu, amax);
   return min(amax < 0x80u ? 127 : max((int)(amax >> 7) - up, least), 253);
 }
-// 16 rows of the tree (group grp).  K side: two e4m3 terms into k1 and k2, the scales of both sides and the bits of bad rows, which the
-// softmax needs.  V side: fp16 into v16.  (Apart, because the V stage may still be read when K is needed.)  Out of line: a
-// few times per CTA.
+// 16 rows of the tree (group grp): K as two e4m3 terms into k1 and k2, V as fp16 into v16, the scales of both (slot 0 of the ring) and the
+// bits of bad rows.  One warp.  Out of line: its registers stay out of the main loop.
 template <int D>
 __device__ __noinline__ void node_group(const bf16* k_nodes, const bf16* v_nodes, long long stride, int n, int grp, uint8_t* k1, uint8_t* k2,
-                                        uint8_t* v16, ScaleRing ring, int slot, uint32_t* s_bad) {
+                                        uint8_t* v16, ScaleRing ring, uint32_t* s_bad) {
   constexpr int RPI = 512 / D, NI = 16 / RPI;
   const int lane = threadIdx.x & 31, ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
-  uint4 x[D / 16];
-  uint32_t bits = node_rows<D>(v_nodes, stride, n, grp, lane, x);
+  uint4 x[D / 16], y[D / 16];
+  load_node_rows<D>(v_nodes, stride, n, grp, lane, x);
+  load_node_rows<D>(k_nodes, stride, n, grp, lane, y);
+  const uint32_t bits = drop_bad_rows<D>(lane, x) | drop_bad_rows<D>(lane, y);
   const int ev = node_exponent(x, 8, 127 - 60);  // (see v_scale_used)
   float inv = __uint_as_float((uint32_t)(254 - ev) << 23);
-  if (v16) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+  for (int i = 0; i < NI; ++i)
 #pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        const uint32_t w[4] = {x[2 * i + k].x, x[2 * i + k].y, x[2 * i + k].z, x[2 * i + k].w};
-        uint32_t h[4];
+    for (int k = 0; k < 2; ++k) {
+      const uint32_t w[4] = {x[2 * i + k].x, x[2 * i + k].y, x[2 * i + k].z, x[2 * i + k].w};
+      uint32_t h[4];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) h[c] = pack_f16(__uint_as_float(w[c] << 16) * inv, __uint_as_float(w[c] & 0xFFFF0000u) * inv);
-        *reinterpret_cast<uint4*>(v16 + sw128_chunk_off(16 * grp + i * RPI + r_in, 2 * ch + k, TC_BN)) = make_uint4(h[0], h[1], h[2], h[3]);
-      }
-    return;
-  }
-  bits |= node_rows<D>(k_nodes, stride, n, grp, lane, x);
-  const int ek = node_exponent(x, 7, 1);
+      for (int c = 0; c < 4; ++c) h[c] = pack_f16(__uint_as_float(w[c] << 16) * inv, __uint_as_float(w[c] & 0xFFFF0000u) * inv);
+      *reinterpret_cast<uint4*>(v16 + sw128_chunk_off(16 * grp + i * RPI + r_in, 2 * ch + k, TC_BN)) = make_uint4(h[0], h[1], h[2], h[3]);
+    }
+  const int ek = node_exponent(y, 7, 1);
   inv = __uint_as_float((uint32_t)(254 - ek) << 23);
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     uint32_t hi[4], lo[4];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
-      const uint32_t w[4] = {x[2 * i + k].x, x[2 * i + k].y, x[2 * i + k].z, x[2 * i + k].w};
+      const uint32_t w[4] = {y[2 * i + k].x, y[2 * i + k].y, y[2 * i + k].z, y[2 * i + k].w};
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         uint16_t h0, l0, h1, l1;
@@ -263,9 +269,9 @@ __device__ __noinline__ void node_group(const bf16* k_nodes, const bf16* v_nodes
     *reinterpret_cast<uint4*>(k2 + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
   }
   if (lane == 0) {
-    ring.ks[slot * 8 + grp] = __uint_as_float((uint32_t)ek << 23);
-    ring.lsv[slot * 8 + grp] = (float)(ev - 127);
-    ring.isv[slot * 8 + grp] = __uint_as_float((uint32_t)(254 - ev) << 23);
+    ring.ks[grp] = __uint_as_float((uint32_t)ek << 23);
+    ring.lsv[grp] = (float)(ev - 127);
+    ring.isv[grp] = __uint_as_float((uint32_t)(254 - ev) << 23);
     if (bits) atomicOr(&s_bad[grp >> 1], bits << (16 * (grp & 1)));
   }
 }
@@ -346,10 +352,12 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   const long long rows_all = (long long)p.total_q * Hq;
 
   const BlockList list = visible_blocks(si.P, p.window, p.sinks, TC_BN);
-  const int total = si.err ? 0 : list.count + (si.n > 0 ? 1 : 0);   // the tree is the last block
+  const int total = si.err ? 0 : list.count + 1;                    // the tree is the first block
   const int per = total / p.num_splits, rem = total % p.num_splits;
   const int blk0 = split * per + min(split, rem);
   const int nb = per + (split < rem ? 1 : 0);
+  const int tree_blocks = nb > 0 && blk0 == 0 ? 1 : 0;              // this CTA's first block is the tree
+  auto prefix_key = [&](int i) { return list.at(blk0 + i - 1) * TC_BN; };  // first key of this CTA's i-th block
   const uint32_t tmem = __shfl_sync(0xffffffffu, *s_tmem, 0);
   const uint32_t tmem_o = tmem + 4 * 64;                            // accumulator of stream t at tmem_o + t * D
 
@@ -361,6 +369,11 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   bool ok = true, compute = false;
 
   if (warp < QT_SOFTMAX / 32) {
+    if (tree_blocks) {
+      const ScaleRing ring = {s_ks, s_lsv, s_isv, s_flag};
+      const long long first = (long long)si.node_base * p.node_stride + g * D;
+      node_group<D>(p.k_nodes + first, p.v_nodes + first, p.node_stride, si.n, warp, sK, sK2, sV, ring, s_bad);
+    }
     // ---- Q: 16-byte pieces, D / 8 lanes to a row, all loads in flight at once -----------------------------------------
     constexpr int LPR = D / 8, RPP = QT_SOFTMAX / LPR, NQ = TC_BM / RPP;
     const int ch = tid % LPR;
@@ -396,6 +409,12 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     mbar_arrive(&s_bar[QB_Q_FULL]);
     asm volatile("bar.sync 3, 320;" ::: "memory");   // the converters have planned the tree, s_qs is complete
     compute = *s_err == 0;
+    if (tree_blocks && tid == 0) {  // every writer has fenced its part before the barrier
+      mbar_arrive(&s_bar[QB_K_FULL0]);
+      mbar_arrive(&s_bar[QB_V_FULL0]);
+      mbar_arrive(&s_bar[QB_V_FULL0]);
+      mbar_arrive(&s_bar[QB_SC0]);
+    }
 
     // ---- softmax --------------------------------------------------------------------------------------------------
     const int R = row0 + row;
@@ -469,16 +488,16 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     };
     // A wait that gives up leaves `ok` false; the loop still runs to its end, so that every barrier gets its arrivals.
     for (int i = 0; i < nb; ++i) {
-      const int at = blk0 + i, group = (i & 3) * 8 + t_mine * 4;
-      const bool is_tree = at >= list.count;
-      const int k0 = (is_tree ? 0 : list.at(at) * TC_BN) + 64 * t_mine;
+      const int group = (i & 3) * 8 + t_mine * 4;
+      const bool is_tree = i < tree_blocks;
+      const int k0 = (is_tree ? 0 : prefix_key(i)) + 64 * t_mine;
       // steps that every row sees whole need no mask
       const bool masked = is_tree || k0 + 64 > si.P || (p.window > 0 && k0 + 64 > p.sinks && si.P + si.n - 1 - k0 >= p.window);
       if (ok) ok = mbar_wait(&s_bar[QB_SC0 + (i & 3)], (i >> 2) & 1, s_abort) &&
-                   mbar_wait(&s_bar[QB_S_FULL00 + 2 * t_mine + (i & 1)], (i >> 1) & 1, s_abort);
+                   mbar_wait(&s_bar[QB_S_FULL0 + (i & 1)], (i >> 1) & 1, s_abort);
       __syncwarp();
       tc_fence_after();
-      const uint32_t s_addr = tmem + lane_base + (2 * t_mine + (i & 1)) * 64;
+      const uint32_t s_addr = tmem + lane_base + (2 * (i & 1) + t_mine) * 64;
       const uint32_t flags = is_tree ? 0u : (s_flag[i & 3] >> (4 * t_mine)) & 15u;   // poisoned 16-key groups of the step
       if (masked || flags) {
         // invisible scores become -inf in tensor memory before the walk
@@ -523,25 +542,25 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     const uint32_t hi8 = D == 128 ? tc_desc_hi(1024) : ((512u >> 4) | (1u << 14) | (4u << 29));
     const uint32_t q_lo = tc_desc_lo(smem_u32(sQ), 16), k_lo = tc_desc_lo(smem_u32(sK), 16), k2_lo = tc_desc_lo(smem_u32(sK2), 16);
     const uint32_t v_lo = tc_desc_lo(smem_u32(sV), TC_BN * 128);
-    const uint32_t idesc_s = tc_idesc_e4m3(TC_BM, 64), idesc_pv = tc_idesc_f16(TC_BM, D, 1);
-    auto issue_s = [&](int t, int i) {
-      if (t == 0) ok = ok && mbar_wait(&s_bar[QB_K_FULL0 + (i & 1)], (i >> 1) & 1, s_abort);  // first reader
+    const uint32_t idesc_s = tc_idesc_e4m3(TC_BM, TC_BN), idesc_pv = tc_idesc_f16(TC_BM, D, 1);
+    auto issue_s = [&](int i) {  // both streams: score buffers 2 (i & 1) and 2 (i & 1) + 1 are neighbours
+      ok = ok && mbar_wait(&s_bar[QB_K_FULL0 + (i & 1)], (i >> 1) & 1, s_abort);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) return;
       tc_fence_after();
-      const uint32_t d = tmem + (2 * t + (i & 1)) * 64;
-      uint32_t kb = k_lo + (i & 1) * (TILE8 >> 4) + t * (64 * D >> 4);
+      const uint32_t d = tmem + (i & 1) * 128;
+      uint32_t kb = k_lo + (i & 1) * (TILE8 >> 4);
       // (Q1 + Q2) K, and for the tree (Q1 + Q2) (K1 + K2); 32 elements a step
-      const int terms = blk0 + i >= list.count ? 2 : 1;
+      const int terms = i < tree_blocks ? 2 : 1;
 #pragma unroll 1
       for (int c = 0; c < terms; ++c) {
 #pragma unroll
         for (int ks = 0; ks < D / 16; ++ks)
           warp_mma_f8(elected, d, q_lo + (ks / (D / 32)) * (TILE8 >> 4) + (ks % (D / 32)) * 2, kb + (ks % (D / 32)) * 2, hi8, idesc_s, c + ks > 0);
-        kb = k2_lo + t * (64 * D >> 4);
+        kb = k2_lo;
       }
-      warp_commit(elected, &s_bar[QB_S_FULL00 + 2 * t + (i & 1)]);
-      if (t == 1) warp_commit(elected, &s_bar[QB_K_EMPTY0 + (i & 1)]);                        // last reader
+      warp_commit(elected, &s_bar[QB_S_FULL0 + (i & 1)]);
+      warp_commit(elected, &s_bar[QB_K_EMPTY0 + (i & 1)]);
     };
     auto issue_pv = [&](int t, int i) {
       ok = ok && mbar_wait(&s_bar[QB_P_FULL00 + 2 * t + (i & 1)], (i >> 1) & 1, s_abort);
@@ -549,7 +568,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) return;
       tc_fence_after();
-      const uint32_t vb = v_lo + (i & 1) * (TILE >> 4) + t * (4 * 2048 >> 4), pb = tmem + (2 * t + (i & 1)) * 64;
+      const uint32_t vb = v_lo + (i & 1) * (TILE >> 4) + t * (4 * 2048 >> 4), pb = tmem + (2 * (i & 1) + t) * 64;
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks)
         warp_mma_ts(elected, tmem_o + t * D, pb + ks * 8, vb + ks * (2048 >> 4), hi, idesc_pv, (i > 0 || ks > 0) ? 1u : 0u);
@@ -559,26 +578,27 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     if (nb > 0) ok = __all_sync(0xffffffffu, mbar_wait(&s_bar[QB_Q_FULL], 0, s_abort));
     // (the first two rounds only issue S; rolled, so that the code is there once)
 #pragma unroll 1
-    for (int it = -4; it < 2 * nb; ++it) {
-      const int i = it >> 1, t = it & 1;
-      if (i >= 0) issue_pv(t, i);
-      if (i + 2 < nb) issue_s(t, i + 2);
+    for (int i = -2; i < nb; ++i) {
+#pragma unroll 1
+      for (int t = 0; t < 2; ++t)
+        if (i >= 0) issue_pv(t, i);
+      if (i + 2 < nb) issue_s(i + 2);
     }
     warp_commit(elected, &s_bar[QB_O_DONE]);
     if (!ok && lane == 0) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
   } else if (warp == QT_LOAD_WARP) {
     // ---- loader: lane l < 8 looks after keys 16 l .. + 15 of every block -----------------------------------------------
-    const int n_cache = max(0, min(nb, list.count - blk0));   // the blocks before the tree
     const bool paged = p.kv.page_size != 0;
     const int page_shift = paged ? 31 - __clz(p.kv.page_size) : 31;
     const int* table = paged ? p.kv.page_table + (long long)b * p.kv.max_pages : nullptr;
-    auto my_key = [&](int j) { return list.at(blk0 + j) * TC_BN + 16 * lane; };
+    auto my_key = [&](int j) { return prefix_key(j) + 16 * lane; };
     auto my_page = [&](int j) {  // page id of this lane's keys, unchecked (nothing waits for it here)
-      if (!paged || lane >= 8 || j >= n_cache || my_key(j) >= si.P) return 0;
+      if (!paged || lane >= 8 || j >= nb || my_key(j) >= si.P) return 0;
       return __ldg(table + (my_key(j) >> page_shift));
     };
-    int page = my_page(0);
-    for (int j = 0; j < n_cache; ++j) {
+    int page = my_page(tree_blocks);
+    for (int j = tree_blocks; j < nb; ++j) {
+      const int r = j - tree_blocks;                            // the stages of V codes are used from the first prefix block on
       const int key = my_key(j);
       const bool on = lane < 8 && key < si.P;
       if (page < 0 || page >= p.kv.num_pages) page = 0;  // reported by the designated CTA; reads stay in the pool
@@ -599,12 +619,12 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       if (lane == 0) mbar_expect_tx(&s_bar[QB_K_FULL0 + (j & 1)], pieces * box_rows * D);
       __syncwarp();
       if (piece) tma_load_4d(smem_u32(sK) + (j & 1) * TILE8 + 16 * lane * D, &kmap, 0, g, c2, c3, &s_bar[QB_K_FULL0 + (j & 1)]);
-      if (j >= 2) ok = ok && mbar_wait(&s_bar[QB_VR_EMPTY0 + (j & 1)], ((j >> 1) - 1) & 1, s_abort);
+      if (r >= 2) ok = ok && mbar_wait(&s_bar[QB_VR_EMPTY0 + (r & 1)], ((r >> 1) - 1) & 1, s_abort);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      if (lane == 0) mbar_expect_tx(&s_bar[QB_VR_FULL0 + (j & 1)], pieces * box_rows * D);
+      if (lane == 0) mbar_expect_tx(&s_bar[QB_VR_FULL0 + (r & 1)], pieces * box_rows * D);
       __syncwarp();
-      if (piece) tma_load_4d(smem_u32(sVr) + (j & 1) * TILE8 + 16 * lane * D, &vmap, 0, g, c2, c3, &s_bar[QB_VR_FULL0 + (j & 1)]);
+      if (piece) tma_load_4d(smem_u32(sVr) + (r & 1) * TILE8 + 16 * lane * D, &vmap, 0, g, c2, c3, &s_bar[QB_VR_FULL0 + (r & 1)]);
       // A NaN scale poisons the rows that see one of its keys; it is noted, and 1 takes its place, so that it meets no other row.
       const uint32_t nan = __ballot_sync(0xffffffffu, ks != ks || vs != vs), tiny = __ballot_sync(0xffffffffu, vs < kMinVScale);
       if (ks != ks || vs != vs) ks = vs = 1.f;
@@ -635,73 +655,51 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       if (grp.tid == 0) *s_err = err;
       asm volatile("bar.sync 3, 320;" ::: "memory");
     }
-    const int cw = warp - QT_CVT_WARP, n_cache = max(0, min(nb, list.count - blk0));
+    const int cw = warp - QT_CVT_WARP;
     constexpr int CPR = D / 16, RPI = 32 / CPR, NI = 32 / RPI;
     const int ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
-    for (int j = 0; j < nb && ok; ++j) {
+    for (int j = tree_blocks; j < nb; ++j) {
+      const int st = (j - tree_blocks) & 1, use = (j - tree_blocks) >> 1;
       uint8_t* stage = sV + (j & 1) * TILE;
-      if (j < n_cache) {
-        ok = mbar_wait(&s_bar[QB_VR_FULL0 + (j & 1)], (j >> 1) & 1, s_abort) && mbar_wait(&s_bar[QB_SC0 + (j & 3)], (j >> 2) & 1, s_abort);
-        if (ok && j >= 2) ok = mbar_wait(&s_bar[QB_V_EMPTY0 + (j & 1)], ((j >> 1) - 1) & 1, s_abort);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) break;
-        const uint8_t* raw = sVr + (j & 1) * TILE8;
-        const int left = si.P - list.at(blk0 + j) * TC_BN;
-        const uint32_t tiny = (s_flag[j & 3] >> 8) & 255u;
+      ok = mbar_wait(&s_bar[QB_VR_FULL0 + st], use & 1, s_abort) && mbar_wait(&s_bar[QB_SC0 + (j & 3)], (j >> 2) & 1, s_abort);
+      if (ok && j >= 2) ok = mbar_wait(&s_bar[QB_V_EMPTY0 + (j & 1)], ((j >> 1) - 1) & 1, s_abort);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) break;
+      const uint8_t* raw = sVr + st * TILE8;
+      const int left = si.P - prefix_key(j);
+      const uint32_t tiny = (s_flag[j & 3] >> 8) & 255u;
 #pragma unroll 1
-        for (int q = 0; q < 2; ++q) {
-          const int r0 = 64 * cw + 32 * q;
-          uint4 x[NI];
+      for (int q = 0; q < 2; ++q) {
+        const int r0 = 64 * cw + 32 * q;
+        uint4 x[NI];
 #pragma unroll
-          for (int i = 0; i < NI; ++i) x[i] = *reinterpret_cast<const uint4*>(raw + code_tile_off<D>(r0 + i * RPI + r_in, ch));
-          if (left < r0 + 32 || tiny) {  // rows past the prefix (stale bytes), and blocks that read as zeros
-#pragma unroll
-            for (int i = 0; i < NI; ++i) {
-              const int r = r0 + i * RPI + r_in;
-              if (r >= left || ((tiny >> (r >> 4)) & 1u)) x[i] = make_uint4(0, 0, 0, 0);
-            }
-          }
+        for (int i = 0; i < NI; ++i) x[i] = *reinterpret_cast<const uint4*>(raw + code_tile_off<D>(r0 + i * RPI + r_in, ch));
+        if (left < r0 + 32 || tiny) {  // rows past the prefix (stale bytes), and blocks that read as zeros
 #pragma unroll
           for (int i = 0; i < NI; ++i) {
-            const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-            uint32_t h[8];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              h[2 * k] = half2_of_e4m3x2((uint16_t)w[k]);
-              h[2 * k + 1] = half2_of_e4m3x2((uint16_t)(w[k] >> 16));
-            }
             const int r = r0 + i * RPI + r_in;
-            *reinterpret_cast<uint4*>(stage + sw128_chunk_off(r, 2 * ch, TC_BN)) = make_uint4(h[0], h[1], h[2], h[3]);
-            *reinterpret_cast<uint4*>(stage + sw128_chunk_off(r, 2 * ch + 1, TC_BN)) = make_uint4(h[4], h[5], h[6], h[7]);
+            if (r >= left || ((tiny >> (r >> 4)) & 1u)) x[i] = make_uint4(0, 0, 0, 0);
           }
         }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(&s_bar[QB_VR_EMPTY0 + (j & 1)]);
-          mbar_arrive(&s_bar[QB_V_FULL0 + (j & 1)]);
-        }
-      } else {  // the tree
-        const ScaleRing ring = {s_ks, s_lsv, s_isv, s_flag};
-        const long long first = (long long)si.node_base * p.node_stride + g * D;
-#pragma unroll 1
-        for (int side = 0; side < 2; ++side) {  // K, V
-          if (j >= 2) ok = ok && mbar_wait(&s_bar[(side ? QB_V_EMPTY0 : QB_K_EMPTY0) + (j & 1)], ((j >> 1) - 1) & 1, s_abort);
-          ok = __all_sync(0xffffffffu, ok);
-          if (ok)
-            for (int grp = 4 * cw; grp < 4 * cw + 4; ++grp)
-              node_group<D>(p.k_nodes + first, p.v_nodes + first, p.node_stride, si.n, grp, sK + (j & 1) * TILE8, sK2, side ? stage : nullptr,
-                            ring, j & 3, s_bad);
-          fence_async_smem();
-          asm volatile("bar.sync 2, 64;" ::: "memory");   // both converter warps
-          if (lane == 0 && ok) {
-            if (side) mbar_arrive(&s_bar[QB_V_FULL0 + (j & 1)]);
-            else if (cw == 0) {
-              mbar_arrive(&s_bar[QB_K_FULL0 + (j & 1)]);
-              mbar_arrive(&s_bar[QB_SC0 + (j & 3)]);
-            }
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          uint32_t h[8];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            h[2 * k] = half2_of_e4m3x2((uint16_t)w[k]);
+            h[2 * k + 1] = half2_of_e4m3x2((uint16_t)(w[k] >> 16));
           }
+          const int r = r0 + i * RPI + r_in;
+          *reinterpret_cast<uint4*>(stage + sw128_chunk_off(r, 2 * ch, TC_BN)) = make_uint4(h[0], h[1], h[2], h[3]);
+          *reinterpret_cast<uint4*>(stage + sw128_chunk_off(r, 2 * ch + 1, TC_BN)) = make_uint4(h[4], h[5], h[6], h[7]);
         }
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive(&s_bar[QB_VR_EMPTY0 + st]);
+        mbar_arrive(&s_bar[QB_V_FULL0 + (j & 1)]);
       }
     }
     if (!ok && lane == 0) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
