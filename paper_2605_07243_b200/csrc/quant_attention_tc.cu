@@ -42,14 +42,16 @@ constexpr int QT_SMALL = 8192;
 constexpr float kQuantLimit = 8192.f; // sum of 32 probabilities relative to the reference beyond which it is raised
 
 enum QtBar { QB_P_FULL00, QB_P_FULL01, QB_P_FULL10, QB_P_FULL11,                              // 128 arrivals: a stream's threads
-             QB_V_FULL0, QB_V_FULL1, QB_VR_EMPTY0, QB_VR_EMPTY1,                              // 2: the converter warps
-             QB_K_FULL0, QB_K_FULL1, QB_VR_FULL0, QB_VR_FULL1, QB_SC0, QB_SC1, QB_SC2, QB_SC3, QB_K_EMPTY0, QB_K_EMPTY1,
+             QB_V_FULL0, QB_V_FULL1, QB_VR_EMPTY0, QB_VR_EMPTY1, QB_VR_EMPTY2,                // 2: the converter warps
+             QB_K_FULL0, QB_K_FULL1, QB_K_FULL2, QB_VR_FULL0, QB_VR_FULL1, QB_VR_FULL2, QB_SC0, QB_SC_LAST = QB_SC0 + 7,
+             QB_K_EMPTY0, QB_K_EMPTY1, QB_K_EMPTY2,
              QB_V_EMPTY0, QB_V_EMPTY1, QB_S_FULL0, QB_S_FULL1, QB_PV0, QB_PV1, QB_O_DONE,
              QB_Q_FULL, QB_COUNT };
 
-// Q terms (2 x 128 D), K codes (2 stages), the tree's second K term, V codes (2 stages), V fp16 (2 stages)
+// Q terms (2 x 128 D), K codes (3 stages), the tree's second K term, V codes (3 stages), V fp16 (2 stages).  Three stages of codes: a
+// stage is free, asked for again and filled within the time of one block less than the ring holds, and a load takes longer than a block.
 template <int D>
-constexpr int quant_tc_smem() { return 1024 + QT_SMALL + TC_BM * D * (2 + 2 + 1 + 2 + 4); }
+constexpr int quant_tc_smem() { return 1024 + QT_SMALL + TC_BM * D * (2 + 3 + 1 + 3 + 4); }
 
 __device__ inline uint32_t tc_idesc_f16(int M, int N, int b_mn_major) {
   return (1u << 4) | ((uint32_t)b_mn_major << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
@@ -92,6 +94,23 @@ __device__ inline void warp_commit(uint32_t elected, uint64_t* bar) {
       "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
       "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}\n" ::"r"(smem_u32(bar)), "r"(elected)
       : "memory");
+}
+// 2^x for two values by the FMA pipe: x = n + f, |f| <= 1/2 (adding 1.5 * 2^23 rounds x to an integer, which the low bits of the sum then
+// hold), 2^f by a polynomial of degree 4 fitted for equal relative error by Remez exchange (2.6e-6), 2^n by the exponent
+// bits.  x <= 100; below -126 the result is 2^-126.
+__device__ inline void exp2_by_fma(float x0, float x1, float& y0, float& y1) {
+  auto both = [](float v) { return pack_f32x2(v, v); };
+  const unsigned long long x = pack_f32x2(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
+  const unsigned long long t = add_f32x2(x, both(12582912.f)), n = add_f32x2(t, both(-12582912.f)), f = fma_f32x2(n, both(-1.f), x);
+  unsigned long long q = fma_f32x2(both(0.009570102f), f, both(0.05591786f));
+  q = fma_f32x2(q, f, both(0.24024744f));
+  q = fma_f32x2(q, f, both(0.6931218f));
+  q = fma_f32x2(q, f, both(0.9999993f));
+  float q0, q1, t0, t1;
+  unpack_f32x2(q, q0, q1);
+  unpack_f32x2(t, t0, t1);
+  y0 = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(t0) << 23));
+  y1 = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23));
 }
 // 32 columns without the wait
 __device__ inline void tmem_ld32_async(uint32_t taddr, uint32_t (&r)[32]) {
@@ -162,8 +181,9 @@ __device__ inline void split_e4m3(float a, float b, uint16_t& hi, uint16_t& lo) 
   lo = e4m3x2_of(a - h.x, b - h.y);
 }
 struct ScaleRing {
-  float *ks, *lsv, *isv;   // [4 slots][8 groups of 16 keys]: K scale, log2 of the V scale, 1 / V scale
-  uint32_t* flag;          // [4 slots]: bits 0-7 the groups with a NaN scale, bits 8-15 those whose V reads as zeros
+  // Eight slots: the loader writes block j's when S of block j - 3 is done, i.e. the softmax with block j - 5.
+  float *ks, *lsv, *isv;   // [8 slots][8 groups of 16 keys]: K scale, log2 of the V scale, 1 / V scale
+  uint32_t* flag;          // [8 slots]: bits 0-7 the groups with a NaN scale, bits 8-15 those whose V reads as zeros
 };
 
 // Lane -> (row, 16-element chunk) when a warp moves rows of D elements, 32 / (D / 16) rows at a time.  D = 128: eight neighbouring
@@ -297,31 +317,32 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   uint32_t* s_anc = reinterpret_cast<uint32_t*>(base);               // 2048 B
   int* s_parent = reinterpret_cast<int*>(base + 2048);               // 512 B
   int* s_depth = reinterpret_cast<int*>(base + 2560);                // 512 B
-  uint64_t* s_bar = reinterpret_cast<uint64_t*>(base + 3072);        // QB_COUNT * 8
+  uint64_t* s_bar = reinterpret_cast<uint64_t*>(base + 4352);        // QB_COUNT * 8 <= 512
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(base + 3328);
   volatile int* s_abort = reinterpret_cast<volatile int*>(base + 3332);   // [0] a wait gave up; [1] the same for the last wait
   int* s_err = reinterpret_cast<int*>(base + 3340);
   uint32_t* s_bad = reinterpret_cast<uint32_t*>(base + 3344);        // [4]: node rows with a NaN or an infinity
-  uint32_t* s_flag = reinterpret_cast<uint32_t*>(base + 3360);       // [4 slots]: 16-key groups of a block with a NaN scale
-  float* s_ks = reinterpret_cast<float*>(base + 3392);               // [4 slots][8 groups of 16 keys] K scale
-  float* s_lsv = s_ks + 32;                                          // log2 of the V scale
-  float* s_isv = s_lsv + 32;                                         // 1 / V scale
+  uint32_t* s_flag = reinterpret_cast<uint32_t*>(base + 3360);       // [8 slots]: see ScaleRing
+  float* s_ks = reinterpret_cast<float*>(base + 7168);               // [8 slots][8 groups of 16 keys] K scale
+  float* s_lsv = s_ks + 64;                                          // log2 of the V scale
+  float* s_isv = s_lsv + 64;                                         // 1 / V scale
   float* s_qs = reinterpret_cast<float*>(base + 3840);               // [128 rows] scale of a Q row
   float* s_ml = reinterpret_cast<float*>(base + 4864);               // [2 streams][reference, sum][128 rows]
   uint8_t* sQ = base + QT_SMALL;      // [2 terms]
-  uint8_t* sK = sQ + 2 * TILE8;       // [2 stages] codes
-  uint8_t* sK2 = sK + 2 * TILE8;      // second term of the tree's K
-  uint8_t* sVr = sK2 + TILE8;         // [2 stages] codes
-  uint8_t* sV = sVr + 2 * TILE8;      // [2 stages] fp16
+  uint8_t* sK = sQ + 2 * TILE8;       // [3 stages] codes
+  uint8_t* sK2 = sK + 3 * TILE8;      // second term of the tree's K
+  uint8_t* sVr = sK2 + TILE8;         // [3 stages] codes
+  uint8_t* sV = sVr + 3 * TILE8;      // [2 stages] fp16
 
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;  // (known to be uniform)
   const int split = blockIdx.x;
   const int Hq = p.tree.n_q_heads, Hkv = p.kv.n_kv_heads, G = p.G;
   if (tid == 0) {
     s_abort[0] = s_abort[1] = 0;
-    for (int i = 0; i < 4; ++i) s_bad[i] = s_flag[i] = 0;
+    for (int i = 0; i < 4; ++i) s_bad[i] = 0;
+    s_flag[0] = 0;
     for (int i = 0; i < QB_COUNT; ++i)
-      mbar_init(&s_bar[i], i <= QB_P_FULL11 ? 128 : i <= QB_VR_EMPTY1 ? 2 : i == QB_Q_FULL ? QT_SOFTMAX : 1);
+      mbar_init(&s_bar[i], i <= QB_P_FULL11 ? 128 : i <= QB_VR_EMPTY2 ? 2 : i == QB_Q_FULL ? QT_SOFTMAX : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == QT_MMA_WARP) {
@@ -470,7 +491,14 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
           unsigned long long sum2[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
-            const float p0 = fast_exp2(d[e]), p1 = fast_exp2(d[e + 1]);
+            // a quarter of the exponentials goes to the FMA pipe: the other pipe's 16 a clock would bound the kernel
+            float p0, p1;
+            if ((e & 7) == 6) {
+              exp2_by_fma(d[e], d[e + 1], p0, p1);
+            } else {
+              p0 = fast_exp2(d[e]);
+              p1 = fast_exp2(d[e + 1]);
+            }
             sum2[e >> 4] = add_f32x2(sum2[e >> 4], pack_f32x2(p0, p1));
             pk[e >> 1] = pack_f16(p0, p1);
           }
@@ -488,17 +516,17 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     };
     // A wait that gives up leaves `ok` false; the loop still runs to its end, so that every barrier gets its arrivals.
     for (int i = 0; i < nb; ++i) {
-      const int group = (i & 3) * 8 + t_mine * 4;
+      const int group = (i & 7) * 8 + t_mine * 4;
       const bool is_tree = i < tree_blocks;
       const int k0 = (is_tree ? 0 : prefix_key(i)) + 64 * t_mine;
       // steps that every row sees whole need no mask
       const bool masked = is_tree || k0 + 64 > si.P || (p.window > 0 && k0 + 64 > p.sinks && si.P + si.n - 1 - k0 >= p.window);
-      if (ok) ok = mbar_wait(&s_bar[QB_SC0 + (i & 3)], (i >> 2) & 1, s_abort) &&
+      if (ok) ok = mbar_wait(&s_bar[QB_SC0 + (i & 7)], (i >> 3) & 1, s_abort) &&
                    mbar_wait(&s_bar[QB_S_FULL0 + (i & 1)], (i >> 1) & 1, s_abort);
       __syncwarp();
       tc_fence_after();
       const uint32_t s_addr = tmem + lane_base + (2 * (i & 1) + t_mine) * 64;
-      const uint32_t flags = is_tree ? 0u : (s_flag[i & 3] >> (4 * t_mine)) & 15u;   // poisoned 16-key groups of the step
+      const uint32_t flags = is_tree ? 0u : (s_flag[i & 7] >> (4 * t_mine)) & 15u;   // poisoned 16-key groups of the step
       if (masked || flags) {
         // invisible scores become -inf in tensor memory before the walk
 #pragma unroll 1
@@ -544,12 +572,12 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     const uint32_t v_lo = tc_desc_lo(smem_u32(sV), TC_BN * 128);
     const uint32_t idesc_s = tc_idesc_e4m3(TC_BM, TC_BN), idesc_pv = tc_idesc_f16(TC_BM, D, 1);
     auto issue_s = [&](int i) {  // both streams: score buffers 2 (i & 1) and 2 (i & 1) + 1 are neighbours
-      ok = ok && mbar_wait(&s_bar[QB_K_FULL0 + (i & 1)], (i >> 1) & 1, s_abort);
+      ok = ok && mbar_wait(&s_bar[QB_K_FULL0 + i % 3], (i / 3) & 1, s_abort);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) return;
       tc_fence_after();
       const uint32_t d = tmem + (i & 1) * 128;
-      uint32_t kb = k_lo + (i & 1) * (TILE8 >> 4);
+      uint32_t kb = k_lo + (i % 3) * (TILE8 >> 4);
       // (Q1 + Q2) K, and for the tree (Q1 + Q2) (K1 + K2); 32 elements a step
       const int terms = i < tree_blocks ? 2 : 1;
 #pragma unroll 1
@@ -560,7 +588,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
         kb = k2_lo;
       }
       warp_commit(elected, &s_bar[QB_S_FULL0 + (i & 1)]);
-      warp_commit(elected, &s_bar[QB_K_EMPTY0 + (i & 1)]);
+      warp_commit(elected, &s_bar[QB_K_EMPTY0 + i % 3]);
     };
     auto issue_pv = [&](int t, int i) {
       ok = ok && mbar_wait(&s_bar[QB_P_FULL00 + 2 * t + (i & 1)], (i >> 1) & 1, s_abort);
@@ -613,31 +641,32 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       const uint32_t pieces = __popc(__ballot_sync(0xffffffffu, piece));
       const int c2 = in_page, c3 = paged ? page : b;
       page = my_page(j + 1);
-      if (j >= 2) ok = ok && mbar_wait(&s_bar[QB_K_EMPTY0 + (j & 1)], ((j >> 1) - 1) & 1, s_abort);
+      const int ks_at = j % 3, vs_at = r % 3;
+      if (j >= 3) ok = ok && mbar_wait(&s_bar[QB_K_EMPTY0 + ks_at], (j / 3 - 1) & 1, s_abort);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      if (lane == 0) mbar_expect_tx(&s_bar[QB_K_FULL0 + (j & 1)], pieces * box_rows * D);
+      if (lane == 0) mbar_expect_tx(&s_bar[QB_K_FULL0 + ks_at], pieces * box_rows * D);
       __syncwarp();
-      if (piece) tma_load_4d(smem_u32(sK) + (j & 1) * TILE8 + 16 * lane * D, &kmap, 0, g, c2, c3, &s_bar[QB_K_FULL0 + (j & 1)]);
-      if (r >= 2) ok = ok && mbar_wait(&s_bar[QB_VR_EMPTY0 + (r & 1)], ((r >> 1) - 1) & 1, s_abort);
+      if (piece) tma_load_4d(smem_u32(sK) + ks_at * TILE8 + 16 * lane * D, &kmap, 0, g, c2, c3, &s_bar[QB_K_FULL0 + ks_at]);
+      if (r >= 3) ok = ok && mbar_wait(&s_bar[QB_VR_EMPTY0 + vs_at], (r / 3 - 1) & 1, s_abort);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
-      if (lane == 0) mbar_expect_tx(&s_bar[QB_VR_FULL0 + (r & 1)], pieces * box_rows * D);
+      if (lane == 0) mbar_expect_tx(&s_bar[QB_VR_FULL0 + vs_at], pieces * box_rows * D);
       __syncwarp();
-      if (piece) tma_load_4d(smem_u32(sVr) + (r & 1) * TILE8 + 16 * lane * D, &vmap, 0, g, c2, c3, &s_bar[QB_VR_FULL0 + (r & 1)]);
+      if (piece) tma_load_4d(smem_u32(sVr) + vs_at * TILE8 + 16 * lane * D, &vmap, 0, g, c2, c3, &s_bar[QB_VR_FULL0 + vs_at]);
       // A NaN scale poisons the rows that see one of its keys; it is noted, and 1 takes its place, so that it meets no other row.
       const uint32_t nan = __ballot_sync(0xffffffffu, ks != ks || vs != vs), tiny = __ballot_sync(0xffffffffu, vs < kMinVScale);
       if (ks != ks || vs != vs) ks = vs = 1.f;
       vs = v_scale_used(vs);
       if (lane < 8) {
-        const int at = (j & 3) * 8 + lane;
+        const int at = (j & 7) * 8 + lane;
         s_ks[at] = ks;
         s_lsv[at] = log2_of_scale(vs);
         s_isv[at] = __fdividef(1.f, vs);
       }
-      if (lane == 0) s_flag[j & 3] = nan | (tiny << 8);
+      if (lane == 0) s_flag[j & 7] = nan | (tiny << 8);
       __syncwarp();
-      if (lane == 0) mbar_arrive(&s_bar[QB_SC0 + (j & 3)]);
+      if (lane == 0) mbar_arrive(&s_bar[QB_SC0 + (j & 7)]);
     }
     if (!ok && lane == 0) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
   } else {
@@ -659,15 +688,15 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     constexpr int CPR = D / 16, RPI = 32 / CPR, NI = 32 / RPI;
     const int ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
     for (int j = tree_blocks; j < nb; ++j) {
-      const int st = (j - tree_blocks) & 1, use = (j - tree_blocks) >> 1;
+      const int st = (j - tree_blocks) % 3, use = (j - tree_blocks) / 3;
       uint8_t* stage = sV + (j & 1) * TILE;
-      ok = mbar_wait(&s_bar[QB_VR_FULL0 + st], use & 1, s_abort) && mbar_wait(&s_bar[QB_SC0 + (j & 3)], (j >> 2) & 1, s_abort);
+      ok = mbar_wait(&s_bar[QB_VR_FULL0 + st], use & 1, s_abort) && mbar_wait(&s_bar[QB_SC0 + (j & 7)], (j >> 3) & 1, s_abort);
       if (ok && j >= 2) ok = mbar_wait(&s_bar[QB_V_EMPTY0 + (j & 1)], ((j >> 1) - 1) & 1, s_abort);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       const uint8_t* raw = sVr + st * TILE8;
       const int left = si.P - prefix_key(j);
-      const uint32_t tiny = (s_flag[j & 3] >> 8) & 255u;
+      const uint32_t tiny = (s_flag[j & 7] >> 8) & 255u;
 #pragma unroll 1
       for (int q = 0; q < 2; ++q) {
         const int r0 = 64 * cw + 32 * q;
