@@ -41,11 +41,11 @@ constexpr int QT_TMEM_COLS = 512;
 constexpr int QT_SMALL = 8192;
 constexpr float kQuantLimit = 8192.f; // sum of 32 probabilities relative to the reference beyond which it is raised
 
-enum QtBar { QB_P_FULL00, QB_P_FULL01, QB_P_FULL10, QB_P_FULL11,                              // 128 arrivals: a stream's threads
+enum QtBar { QB_P_FULL0, QB_P_FULL1,                                                          // 8 arrivals: the softmax warps
              QB_V_FULL0, QB_V_FULL1, QB_VR_EMPTY0, QB_VR_EMPTY1, QB_VR_EMPTY2,                // 2: the converter warps
              QB_K_FULL0, QB_K_FULL1, QB_K_FULL2, QB_VR_FULL0, QB_VR_FULL1, QB_VR_FULL2, QB_SC0, QB_SC_LAST = QB_SC0 + 7,
              QB_K_EMPTY0, QB_K_EMPTY1, QB_K_EMPTY2,
-             QB_V_EMPTY0, QB_V_EMPTY1, QB_S_FULL0, QB_S_FULL1, QB_PV0, QB_PV1, QB_O_DONE,
+             QB_V_EMPTY0, QB_V_EMPTY1, QB_S_FULL0, QB_S_FULL1, QB_PV, QB_O_DONE,
              QB_Q_FULL, QB_COUNT };
 
 // Q terms (2 x 128 D), K codes (3 stages), the tree's second K term, V codes (3 stages), V fp16 (2 stages).  Three stages of codes: a
@@ -342,7 +342,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     for (int i = 0; i < 4; ++i) s_bad[i] = 0;
     s_flag[0] = 0;
     for (int i = 0; i < QB_COUNT; ++i)
-      mbar_init(&s_bar[i], i <= QB_P_FULL11 ? 128 : i <= QB_VR_EMPTY2 ? 2 : i == QB_Q_FULL ? QT_SOFTMAX : 1);
+      mbar_init(&s_bar[i], i <= QB_P_FULL1 ? 8 : i <= QB_VR_EMPTY2 ? 2 : i == QB_Q_FULL ? QT_SOFTMAX : 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == QT_MMA_WARP) {
@@ -482,7 +482,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
             l_run *= factor;
             // the accumulator holds the steps before this one: the last of them may still be under way
             if (i > 0) {
-              if (ok) ok = mbar_wait(&s_bar[QB_PV0 + t_mine], (i - 1) & 1, s_abort);
+              if (ok) ok = mbar_wait(&s_bar[QB_PV], (i - 1) & 1, s_abort);
               __syncwarp();
               tc_fence_after();
             }
@@ -554,7 +554,8 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       walk(i, group, s_addr);
       tmem_wait_st();
       tc_fence_before();
-      mbar_arrive(&s_bar[QB_P_FULL00 + 2 * t_mine + (i & 1)]);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s_bar[QB_P_FULL0 + (i & 1)]);
     }
     if (!ok) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
     if (poison) l_run = __uint_as_float(0x7FC00000u);
@@ -590,26 +591,25 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       warp_commit(elected, &s_bar[QB_S_FULL0 + (i & 1)]);
       warp_commit(elected, &s_bar[QB_K_EMPTY0 + i % 3]);
     };
-    auto issue_pv = [&](int t, int i) {
-      ok = ok && mbar_wait(&s_bar[QB_P_FULL00 + 2 * t + (i & 1)], (i >> 1) & 1, s_abort);
-      if (t == 0) ok = ok && mbar_wait(&s_bar[QB_V_FULL0 + (i & 1)], (i >> 1) & 1, s_abort);
+    auto issue_pv = [&](int i) {
+      ok = ok && mbar_wait(&s_bar[QB_V_FULL0 + (i & 1)], (i >> 1) & 1, s_abort) && mbar_wait(&s_bar[QB_P_FULL0 + (i & 1)], (i >> 1) & 1, s_abort);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) return;
       tc_fence_after();
-      const uint32_t vb = v_lo + (i & 1) * (TILE >> 4) + t * (4 * 2048 >> 4), pb = tmem + (2 * (i & 1) + t) * 64;
+      const uint32_t vb = v_lo + (i & 1) * (TILE >> 4), pb = tmem + (i & 1) * 128;
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-        warp_mma_ts(elected, tmem_o + t * D, pb + ks * 8, vb + ks * (2048 >> 4), hi, idesc_pv, (i > 0 || ks > 0) ? 1u : 0u);
-      warp_commit(elected, &s_bar[QB_PV0 + t]);
-      if (t == 1) warp_commit(elected, &s_bar[QB_V_EMPTY0 + (i & 1)]);
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks)
+          warp_mma_ts(elected, tmem_o + t * D, pb + t * 64 + ks * 8, vb + (t * 4 + ks) * (2048 >> 4), hi, idesc_pv, (i > 0 || ks > 0) ? 1u : 0u);
+      warp_commit(elected, &s_bar[QB_PV]);
+      warp_commit(elected, &s_bar[QB_V_EMPTY0 + (i & 1)]);
     };
     if (nb > 0) ok = __all_sync(0xffffffffu, mbar_wait(&s_bar[QB_Q_FULL], 0, s_abort));
     // (the first two rounds only issue S; rolled, so that the code is there once)
 #pragma unroll 1
     for (int i = -2; i < nb; ++i) {
-#pragma unroll 1
-      for (int t = 0; t < 2; ++t)
-        if (i >= 0) issue_pv(t, i);
+      if (i >= 0) issue_pv(i);
       if (i + 2 < nb) issue_s(i + 2);
     }
     warp_commit(elected, &s_bar[QB_O_DONE]);
