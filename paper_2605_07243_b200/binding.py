@@ -540,32 +540,37 @@ class _PageArray(C.Structure):
     _fields_ = [("base", C.c_void_p), ("page_bytes", C.c_int64), ("layer_stride", C.c_int64)]
 
 
-def _addr(t, dtype, device, numel=None):
-    """Address of a contiguous tensor of this type on this device (None: a null pointer)."""
-    if t is None:
-        return None
+def _refuse(t, dtype, device, numel):
     if t.dtype != dtype:
         raise TypeError(f"expected {dtype}, got {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"expected a tensor on {device}, got {t.device}")
+    if t.get_device() != device:
+        raise ValueError(f"expected a tensor on {'the CPU' if device < 0 else f'cuda:{device}'}, got {t.device}")
     if not t.is_contiguous():
         raise ValueError("expected a contiguous tensor")
-    if numel is not None and t.numel() != numel:
-        raise ValueError(f"expected {numel} elements, got {tuple(t.shape)}")
+    raise ValueError(f"expected {numel} elements, got {tuple(t.shape)}")
+
+
+def _addr(t, dtype, device, numel=None):
+    """Address of a contiguous tensor of this type on this device (its index, -1 for the CPU); None: a null pointer."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous() or (numel is not None and t.numel() != numel):
+        _refuse(t, dtype, device, numel)
     return t.data_ptr()
 
 
 def _cuda_device(t):
-    """The tensor's device, which has to be the current one: the library enqueues on the current device's stream."""
-    if not t.is_cuda:
+    """Index of the tensor's device, which has to be the current one: the library enqueues on the current device's stream."""
+    dev = t.get_device()
+    if dev < 0:
         raise ValueError("expected a CUDA tensor")
-    if t.device.index != torch.cuda.current_device():
+    if dev != torch.cuda.current_device():
         raise ValueError(f"tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return t.device
+    return dev
 
 
-def _stream_of(device):
-    return torch.cuda.current_stream(device).cuda_stream
+# The current stream's handle without building a Stream object for every call, where torch has that.
+_stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
 
 
 @dataclass(frozen=True)
@@ -588,7 +593,7 @@ class QuantCache:
 
     def __post_init__(self):
         s = _QuantCache()
-        dev = self.k_codes.device
+        dev = self.k_codes.get_device()
         lead = self.k_codes.shape[:-2]
         if self.k_codes.dim() != (4 if self.n_layers == 1 and self.k_codes.dim() == 4 else 5):
             raise ValueError("codes must be [(layers,) rows, tokens, n_kv_heads, head_dim]")
@@ -621,6 +626,7 @@ class QuantCache:
         object.__setattr__(self, "c_struct", s)
         object.__setattr__(self, "c_ref", C.addressof(s))
         object.__setattr__(self, "batch", int(s.batch))
+        object.__setattr__(self, "device", dev)
 
 
 @dataclass(frozen=True)
@@ -635,7 +641,7 @@ class QuantTree:
 
     def __post_init__(self):
         s = _QuantTree()
-        dev = self.prefix_len.device
+        dev = self.prefix_len.get_device()
         s.n_q_heads, s.total_nodes = self.n_q_heads, self.parent.numel()
         s.max_nodes, s.max_prefix = self.max_nodes, self.max_prefix
         s.prefix_len = _addr(self.prefix_len, torch.int32, dev)
@@ -643,18 +649,26 @@ class QuantTree:
         s.parent = _addr(self.parent, torch.int32, dev)
         object.__setattr__(self, "c_struct", s)
         object.__setattr__(self, "c_ref", C.addressof(s))
+        object.__setattr__(self, "device", dev)
+        object.__setattr__(self, "batch", self.prefix_len.numel())
+        object.__setattr__(self, "total_nodes", self.parent.numel())
 
 
 def _rows_of(t, heads, dim, device, what):
     """(address, elements between rows) of bf16 rows [..., heads, dim] whose rows are contiguous inside: a whole tensor or
     a slice of a fused projection."""
-    if t.dtype != torch.bfloat16:
+    if t.dtype is not torch.bfloat16:
         raise TypeError(f"{what}: expected torch.bfloat16, got {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{what}: expected a tensor on {device}, got {t.device}")
-    shape, stride = t.shape, t.stride()
-    if shape[-2] != heads or shape[-1] != dim or stride[-1] != 1 or (heads > 1 and stride[-2] != dim):
-        raise ValueError(f"{what}: expected rows of [{heads}, {dim}] that are contiguous inside, got {tuple(shape)} with strides {stride}")
+    if t.get_device() != device:
+        raise ValueError(f"{what}: expected a tensor on cuda:{device}, got {t.device}")
+    shape = t.shape
+    if len(shape) < 3 or shape[-2] != heads or shape[-1] != dim:
+        raise ValueError(f"{what}: expected rows of [{heads}, {dim}], got {tuple(shape)}")
+    if t.is_contiguous():
+        return t.data_ptr(), heads * dim
+    stride = t.stride()
+    if stride[-1] != 1 or (heads > 1 and stride[-2] != dim):
+        raise ValueError(f"{what}: expected rows that are contiguous inside, got strides {stride}")
     return t.data_ptr(), (stride[-3] if shape[-3] > 1 else heads * dim)
 
 
@@ -672,12 +686,12 @@ def sb_tree_attention_quant(kv: QuantCache, tree: QuantTree, q, k_nodes, v_nodes
     dev = _cuda_device(q)
     total_q = q.shape[0]
     Hq, D, B = tree.n_q_heads, kv.head_dim, kv.batch
-    if tree.prefix_len.numel() != B:
+    if tree.batch != B:
         raise ValueError("the tree batch and the cache have different numbers of sequences")
-    if kv.k_codes.device != dev or tree.parent.device != dev:
-        raise ValueError(f"cache, tree and q must all be on {dev}")
+    if kv.device != dev or tree.device != dev:
+        raise ValueError(f"cache, tree and q must all be on cuda:{dev}")
     q_ptr, q_stride = _rows_of(q, Hq, D, dev, "q")
-    total = tree.parent.numel()
+    total = tree.total_nodes
     if k_nodes.shape[0] != total or v_nodes.shape[0] != total:
         raise ValueError(f"k_nodes and v_nodes must have {total} rows")
     k_ptr, k_stride = _rows_of(k_nodes, kv.n_kv_heads, D, dev, "k_nodes")
@@ -709,8 +723,8 @@ def sb_kv_append_quant(kv: QuantCache, k_rows, v_rows, row_offsets, length, *, m
     row_offsets[b] .. row_offsets[b+1] - 1, or with path_nodes and accept_len (as sb_verify_accept leaves them) the accepted
     path's rows.  max_rows bounds the rows of a sequence.  -> (new_len [B], status [B])."""
     dev = _cuda_device(k_rows)
-    if kv.k_codes.device != dev:
-        raise ValueError(f"cache and rows must both be on {dev}")
+    if kv.device != dev:
+        raise ValueError(f"cache and rows must both be on cuda:{dev}")
     B = kv.batch
     if k_rows.shape != v_rows.shape or k_rows.stride() != v_rows.stride():
         raise ValueError("k_rows and v_rows must have the same shape and strides")
@@ -748,7 +762,7 @@ class PagePool:
 
     def __post_init__(self):
         s = _PagePool()
-        dev = self.page_table.device
+        dev = self.page_table.get_device()
         if self.page_table.dim() != 2:
             raise ValueError("page_table must be [slots, max_pages]")
         s.page_size, s.num_pages = self.page_size, self.refs.numel()
@@ -758,6 +772,7 @@ class PagePool:
         s.refs = _addr(self.refs, torch.int32, dev)
         object.__setattr__(self, "c_struct", s)
         object.__setattr__(self, "c_ref", C.addressof(s))
+        object.__setattr__(self, "device", dev)
 
     @classmethod
     def empty(cls, n_slots, max_pages, num_pages, page_size, device="cuda"):
@@ -795,9 +810,10 @@ class PageArrays:
             if tuple(lead) != (self.n_layers, self.num_pages):
                 raise ValueError(f"expected [{self.n_layers}, {self.num_pages}, ...] (or without layers), got {tuple(t.shape)}")
             layer = t.numel() // self.n_layers * t.element_size()
-            a.base, a.page_bytes, a.layer_stride = _addr(t, t.dtype, self.tensors[0].device), layer // self.num_pages, layer
+            a.base, a.page_bytes, a.layer_stride = _addr(t, t.dtype, self.tensors[0].get_device()), layer // self.num_pages, layer
         object.__setattr__(self, "c_array", arr)
         object.__setattr__(self, "c_ref", C.addressof(arr))
+        object.__setattr__(self, "device", self.tensors[0].get_device())
 
 
 def sb_pages_workspace_bytes(pool: PagePool, n: int) -> int:
@@ -858,8 +874,8 @@ def sb_pages_compact(pool: PagePool, copies: PageCopies, *, n_used=None, workspa
 def sb_pages_copy(arrays: PageArrays, copies: PageCopies):
     """Copies the contents of the pages in `copies`, every layer of every array, in one launch."""
     dev = _cuda_device(copies.src)
-    if arrays.tensors[0].device != dev:
-        raise ValueError(f"expected arrays on {dev}")
+    if arrays.device != dev:
+        raise ValueError(f"expected arrays on cuda:{dev}")
     rc = load().sb_pages_copy(arrays.c_ref, len(arrays.tensors), arrays.n_layers, arrays.num_pages, _addr(copies.src, torch.int32, dev),
                               _addr(copies.dst, torch.int32, dev, copies.src.numel()), _addr(copies.count, torch.int32, dev, 1),
                               copies.src.numel(), _stream_of(dev))

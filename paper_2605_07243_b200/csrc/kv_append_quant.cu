@@ -47,7 +47,7 @@ __device__ inline uint2 codes_times(const uint4& x, float f) {
   for (int k = 0; k < 4; ++k) c[k] = e4m3x2_of(__uint_as_float(w[k] << 16) * f, __uint_as_float(w[k] & 0xFFFF0000u) * f);
   return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
 }
-__device__ __noinline__ uint2 codes_over(uint4 x, float s) {
+static __device__ __noinline__ uint2 codes_over(uint4 x, float s) {
   const uint32_t w[4] = {x.x, x.y, x.z, x.w};
   uint32_t c[4];
 #pragma unroll
@@ -55,7 +55,7 @@ __device__ __noinline__ uint2 codes_over(uint4 x, float s) {
   return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
 }
 // Eight codes under another scale.
-__device__ __noinline__ uint2 rescaled(uint2 v, float old, float s) {
+static __device__ __noinline__ uint2 rescaled(uint2 v, float old, float s) {
   const uint32_t w[2] = {v.x, v.y};
   uint32_t out[2];
 #pragma unroll

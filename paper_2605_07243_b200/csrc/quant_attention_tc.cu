@@ -137,7 +137,7 @@ __device__ inline void tmem_wait_ld(uint32_t (&r)[32]) {
 // Rescales a row in tensor memory: its accumulator (unless there is none yet) and the quarters of P already written
 // for the present block.  Rare, and out of line: its registers and code stay out of the main loop.
 template <int D>
-__device__ __noinline__ void rescale_row(uint32_t o_addr, uint32_t p_addr, int quarters, float factor) {
+static __device__ __noinline__ void rescale_row(uint32_t o_addr, uint32_t p_addr, int quarters, float factor) {
   tmem_wait_st();  // what is read back was written by this thread
   if (o_addr != 0xffffffffu) {
 #pragma unroll 1
@@ -247,7 +247,7 @@ __device__ inline int node_exponent(const uint4 (&x)[N], int up, int least) {
 // 16 rows of the tree (group grp): K as two e4m3 terms into k1 and k2, V as fp16 into v16, the scales of both (slot 0 of the ring) and the
 // bits of bad rows.  One warp.  Out of line: its registers stay out of the main loop.
 template <int D>
-__device__ __noinline__ void node_group(const bf16* k_nodes, const bf16* v_nodes, long long stride, int n, int grp, uint8_t* k1, uint8_t* k2,
+static __device__ __noinline__ void node_group(const bf16* k_nodes, const bf16* v_nodes, long long stride, int n, int grp, uint8_t* k1, uint8_t* k2,
                                         uint8_t* v16, ScaleRing ring, uint32_t* s_bad) {
   constexpr int RPI = 512 / D, NI = 16 / RPI;
   const int lane = threadIdx.x & 31, ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
@@ -297,7 +297,7 @@ __device__ __noinline__ void node_group(const bf16* k_nodes, const bf16* v_nodes
 }
 
 // Scores of 32 columns whose bit is not set become -inf.
-__device__ __noinline__ void mask_scores(uint32_t addr, uint32_t word) {
+static __device__ __noinline__ void mask_scores(uint32_t addr, uint32_t word) {
   uint32_t x[32];
   tmem_ld32(addr, x);
 #pragma unroll
