@@ -102,7 +102,7 @@ static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree,
   }
   // Chunks per (sequence, KV head): enough for two CTAs on every SM, grouped into clusters of up to 8.
   pl.grid_tiles = ceil_div(rows, 16);
-  const int groups = (int)((keys + 31) / 32) + (window > 0 ? 2 : 0) + ceil_div(tree->max_nodes, 32);
+  const int groups = (int)((keys + 31) / 32) + (window > 0 ? 2 : 0) + ceil_div(tree->max_nodes, 16);
   const long long units = (long long)kv->batch * kv->n_kv_heads * pl.grid_tiles;
   int s;
   if (num_splits > 0) {

@@ -2,8 +2,8 @@
 // sliding window, and the list of key blocks that a sequence's nodes can see.
 #pragma once
 
-#include "attention_common.cuh"
 #include "quant_common.cuh"
+#include "tc_common.cuh"
 
 namespace sb {
 
@@ -99,20 +99,25 @@ __device__ inline BlockList visible_blocks(int P, int window, int sinks, int siz
   return l;
 }
 
-// Sequence with rank z by length, longest first (see sequence_of_rank in attention_common.cuh).
-__device__ inline int quant_sequence_of_rank(const QuantAttnParams& p, int z, int* s_len, int* s_perm) {
+// Sequence with rank z by length, longest first (see sequence_of_rank in attention_common.cuh).  batch <= SB_MAX_NODES; s_len: 16-byte
+// aligned scratch of SB_MAX_NODES ints, s_pick: one int.
+__device__ inline int quant_sequence_of_rank(const QuantAttnParams& p, int z, int* s_len, int* s_pick) {
   const int B = p.kv.batch, tid = threadIdx.x;
-  for (int i = tid; i < B; i += blockDim.x)
-    s_len[i] = p.tree.prefix_len[i];
+  for (int i = tid; i < SB_MAX_NODES; i += blockDim.x) s_len[i] = i < B ? p.tree.prefix_len[i] : (int)0x80000000;
   __syncthreads();
   for (int i = tid; i < B; i += blockDim.x) {
     const int me = s_len[i];
     int r = 0;
-    for (int j = 0; j < B; ++j) r += (s_len[j] > me || (s_len[j] == me && j < i)) ? 1 : 0;
-    s_perm[r] = i;
+#pragma unroll 4
+    for (int j = 0; j < B; j += 4) {
+      const int4 o = *reinterpret_cast<const int4*>(s_len + j);
+      r += (o.x > me || (o.x == me && j < i)) + (o.y > me || (o.y == me && j + 1 < i)) + (o.z > me || (o.z == me && j + 2 < i)) +
+           (o.w > me || (o.w == me && j + 3 < i));
+    }
+    if (r == z) *s_pick = i;
   }
   __syncthreads();
-  const int b = s_perm[z];
+  const int b = *s_pick;
   __syncthreads();
   return b;
 }
@@ -124,6 +129,27 @@ __device__ inline float v_scale_used(float s) { return s < kMinVScale ? kMinVSca
 // bf16 magnitudes >= 0x7F80 are NaN or infinite
 __device__ inline bool bf16x2_nonfinite(uint32_t w) {
   return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
+}
+
+// Tensor maps of the codes: rank-4 view (d, KV head, row, page); a contiguous cache is one "page" of kv_capacity rows per sequence.  A box is
+// one head's D bytes of *box_rows rows (a page's, at most `most`), swizzled by its row size.
+template <int D>
+inline sb_status make_code_maps(const QuantAttnParams& p, int most, CUtensorMap* kmap, CUtensorMap* vmap, int* box_rows) {
+  *box_rows = p.kv.page_size == 0 || p.kv.page_size > most ? most : p.kv.page_size;
+  EncodeTiledFn enc = encode_tiled_fn();
+  if (!enc) return SB_ERR_CUDA;
+  const uint8_t* codes[2] = {p.k_codes, p.v_codes};
+  for (int i = 0; i < 2; ++i) {
+    const cuuint64_t H = (cuuint64_t)p.kv.n_kv_heads, rows = (cuuint64_t)(p.kv.page_size == 0 ? p.kv.kv_capacity : p.kv.page_size);
+    const cuuint64_t dims[4] = {(cuuint64_t)D, H, rows, (cuuint64_t)(p.kv.page_size == 0 ? p.kv.batch : p.kv.num_pages)};
+    const cuuint64_t strides[3] = {(cuuint64_t)D, H * D, rows * H * D};
+    const cuuint32_t box[4] = {(cuuint32_t)D, 1, (cuuint32_t)*box_rows, 1}, elem[4] = {1, 1, 1, 1};
+    if (enc(i ? vmap : kmap, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<uint8_t*>(codes[i]), dims, strides, box, elem,
+            CU_TENSOR_MAP_INTERLEAVE_NONE, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+      return SB_ERR_UNSUPPORTED;  // an extent or stride beyond what a tensor map holds
+  }
+  return SB_OK;
 }
 
 constexpr int kQuantMaxCluster = 8;

@@ -28,7 +28,6 @@
 // else, scaled by a power of two per 16 rows as if they were codes (K as two e4m3 terms, V as fp16).  Then come the prefix
 // blocks of 128 keys that the window leaves.
 #include "quant_attention.cuh"
-#include "tc_common.cuh"
 
 namespace sb {
 
@@ -173,12 +172,6 @@ __device__ inline float log2_of_scale(float s) {
 template <int D>
 __device__ inline uint32_t code_tile_off(int r, int ch) {
   return (uint32_t)(r * D + ((ch ^ (D == 128 ? (r & 7) : ((r >> 1) & 3))) << 4));
-}
-// Two values -> e4m3 codes of the nearest values and of what is left.
-__device__ inline void split_e4m3(float a, float b, uint16_t& hi, uint16_t& lo) {
-  hi = e4m3x2_of(a, b);
-  const float2 h = float2_of_e4m3x2(hi);
-  lo = e4m3x2_of(a - h.x, b - h.y);
 }
 struct ScaleRing {
   // Eight slots: the loader writes block j's when S of block j - 3 is done, i.e. the softmax with block j - 5.
@@ -846,22 +839,10 @@ static sb_status launch_quant_tc_d(const QuantAttnParams& p, dim3 grid, cudaStre
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  // rank-4 view (d, KV head, row, page) of the codes; a contiguous cache is one "page" of kv_capacity rows per sequence
-  const int box_rows = p.kv.page_size == 0 || p.kv.page_size > TC_BN ? TC_BN : p.kv.page_size;
   CUtensorMap kmap, vmap;
-  const uint8_t* codes[2] = {p.k_codes, p.v_codes};
-  EncodeTiledFn enc = encode_tiled_fn();
-  if (!enc) return SB_ERR_CUDA;
-  for (int i = 0; i < 2; ++i) {
-    const cuuint64_t H = (cuuint64_t)p.kv.n_kv_heads, rows = (cuuint64_t)(p.kv.page_size == 0 ? p.kv.kv_capacity : p.kv.page_size);
-    const cuuint64_t dims[4] = {(cuuint64_t)D, H, rows, (cuuint64_t)(p.kv.page_size == 0 ? p.kv.batch : p.kv.num_pages)};
-    const cuuint64_t strides[3] = {(cuuint64_t)D, H * D, rows * H * D};
-    const cuuint32_t box[4] = {(cuuint32_t)D, 1, (cuuint32_t)box_rows, 1}, elem[4] = {1, 1, 1, 1};
-    if (enc(i ? &vmap : &kmap, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<uint8_t*>(codes[i]), dims, strides, box, elem,
-            CU_TENSOR_MAP_INTERLEAVE_NONE, D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
-            CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-      return SB_ERR_UNSUPPORTED;  // an extent or stride beyond what a tensor map holds
-  }
+  int box_rows;
+  const sb_status ms = make_code_maps<D>(p, TC_BN, &kmap, &vmap, &box_rows);
+  if (ms != SB_OK) return ms;
   if (cudaLaunchKernelEx(&cfg, quant_tc_kernel<D>, p, kmap, vmap, box_rows) != cudaSuccess) {
     cudaGetLastError();
     return SB_ERR_CUDA;

@@ -38,6 +38,13 @@ __device__ inline float2 float2_of_e4m3x2(uint16_t c) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
+// Two values -> e4m3 codes of the nearest values and of what is left.
+__device__ inline void split_e4m3(float a, float b, uint16_t& hi, uint16_t& lo) {
+  hi = e4m3x2_of(a, b);
+  const float2 h = float2_of_e4m3x2(hi);
+  lo = e4m3x2_of(a - h.x, b - h.y);
+}
+
 inline sb_status check_quant_cache(const sb_quant_cache* kv) {
   if (!kv || kv->batch < 1 || kv->n_kv_heads < 1 || !kv->k_codes || !kv->v_codes || !kv->k_scale || !kv->v_scale ||
       kv->n_layers < 1 || kv->codes_layer_stride < 0 || kv->codes_layer_stride % 16 != 0 || kv->scale_layer_stride < 0)
