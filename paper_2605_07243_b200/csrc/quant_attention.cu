@@ -84,14 +84,14 @@ static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree,
     pl.grid_tiles = ceil_div(rows, 128);
     const int blocks = (int)((keys + 127) / 128) + (window > 0 ? 2 : 0) + 1;
     const long long units = (long long)kv->batch * kv->n_kv_heads * pl.grid_tiles;
-    const double per_block = 1.2, fixed = 6.0;
+    const double per_block = 1.28, fixed = 10.0;  // us: one 60-node tree over 2k tokens by 1, 2, 3, 6, 9 chunks: 38, 30, 26, 22, 23
     const double partial = 2.0 * (double)total_q * tree->n_q_heads * kv->head_dim * 2.0 / 5e6;
     int best = 1;
     double best_cost = 0.0;
     const int most = num_splits > 0 ? 1 : (blocks < 64 ? blocks : 64);
     for (int s = 1; s <= most; ++s) {
       const long long waves = (units * s + sms - 1) / sms;
-      const double cost = (double)waves * (ceil_div(blocks, s) * per_block + fixed) + (s > 1 ? partial * s + 3.0 : 0.0);
+      const double cost = (double)waves * (ceil_div(blocks, s) * per_block + fixed) + (s > 1 ? partial * s + 1.0 + 0.5 * s : 0.0);
       if (s == 1 || cost < best_cost) {
         best = s;
         best_cost = cost;
@@ -100,7 +100,11 @@ static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree,
     pl.outer = num_splits > 0 ? (num_splits < blocks ? num_splits : blocks) : best;
     return pl;
   }
-  // Chunks per (sequence, KV head): enough for two CTAs on every SM, grouped into clusters of up to 8.
+  // Chunks per (sequence, KV head, tile), grouped into clusters of up to 8.  About 520 CTAs measured best (three fit on an SM; ragged
+  // 4k prefixes, 8 KV heads, us by 1 / 2 / 3 / 4 / 6 / 8 chunks: 8 sequences 113 / 62 / 49 / 39 / 37 / 35, 16: 115 / 71 / 61 / 51 /
+  // 54 / 64, 32: 150 / 89 / 89 / 94 / 103 / 124, 64: 159 / 138 / 156 / 164 / 183 / 227, 128: 263 / 285 / 329): a chunk per CTA
+  // alone is bound by its own latency, every further CTA costs its start and its merge.  More than 8 chunks need the merge kernel, which
+  // pays from about 5k keys on (32k: 67 us by 8, 29 by 32); then one wave of two CTAs per SM.
   pl.grid_tiles = ceil_div(rows, 16);
   const int groups = (int)((keys + 31) / 32) + (window > 0 ? 2 : 0) + ceil_div(tree->max_nodes, 16);
   const long long units = (long long)kv->batch * kv->n_kv_heads * pl.grid_tiles;
@@ -108,14 +112,18 @@ static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree,
   if (num_splits > 0) {
     s = num_splits;
   } else {
-    s = (int)(2LL * sms / units);
+    s = (int)((520 + units - 1) / units);
     const int most = ceil_div(groups, 4);  // a group for each of the four warps
     if (s > most) s = most;
-    if (s > 64) s = 64;
+    if (s > kQuantMaxCluster) {
+      s = groups > 160 ? (int)(2LL * sms / units) : kQuantMaxCluster;
+      s = s < kQuantMaxCluster ? kQuantMaxCluster : (s > 64 ? 64 : s / kQuantMaxCluster * kQuantMaxCluster);
+    } else if (s == 5 || s == 7) {
+      --s;                                 // rows divide evenly among 4 or 6
+    }
   }
   if (s > groups) s = groups;
   if (s < 1) s = 1;
-  if (s > kQuantMaxCluster && num_splits == 0) s = s / kQuantMaxCluster * kQuantMaxCluster;
   for (int c = kQuantMaxCluster; c >= 1; --c)
     if (s % c == 0) { pl.cluster = c; break; }
   pl.outer = s / pl.cluster;
