@@ -76,22 +76,37 @@ static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree,
   long long keys = tree->max_prefix;  // visible ones, at most
   if (window > 0 && (long long)window + sinks + 64 < keys) keys = (long long)window + sinks + 64;
   const int sms = quant_num_sms();
-  pl.tc = rows > 16;
+  // The 16-row kernel starts and ends in half the time (8 us against 15), but walks the keys once per 16 rows, with the slower matrix
+  // instructions.  us by it and by the tcgen05 kernel, 8 KV heads, groups of 4: 1 to 4 nodes (one tile), 2k keys 11.7 / 20, 64 ragged 8k
+  // prefixes 143 / 242; 16 nodes over 128, 512, 2k keys 10 / 14, 11 / 16, 14 / 20; 32 nodes 11 / 14, 13 / 16.5, 19 / 20.5; 60 nodes
+  // 13 / 14, 17 / 17, 29 / 22; 5 to 8 nodes, 4 ragged 8k prefixes 37 / 36, 16 of them 84 / 74, 64 of them 232 / 209.
+  const long long tiles = (long long)kv->batch * kv->n_kv_heads * ceil_div(rows, 16);
+  pl.tc = rows > 16 && (tiles > 64 || tiles * keys > (1 << 17));
   pl.cluster = 1;
   if (pl.tc) {
-    // CTAs run in waves of one per SM.  A CTA costs its key blocks plus a fixed start and end; every chunk beyond the first writes
-    // and re-reads bf16 partials of all rows, and the merge is one more kernel.
+    // A CTA costs its key blocks plus a fixed start and end.  CTAs start longest first on whichever SM is free: equal ones run in waves,
+    // ragged ones (three quarters of the longest, taken on average) end about half a chunk unevenly; the estimate lies between the two.
+    // Every chunk beyond the first writes and re-reads bf16 partials of all rows, and the merge is one more kernel.  us by 1 / 2 / 3 / 4 /
+    // 6 chunks: one 60-node tree over 2k keys 38 / 30 / 26 / 24 / 22; 8-node trees over ragged 8k prefixes, 4 of them 89 / 54 / 42 / 37 /
+    // 40, 16: 91 / 74 / 82 / 89 / 104, 64: 209 / 244 / 273 / 299 / 355; four full trees, 64 heads, over 32k keys 695 / 724 / 725 / 690 / 772.
     pl.grid_tiles = ceil_div(rows, 128);
     const int blocks = (int)((keys + 127) / 128) + (window > 0 ? 2 : 0) + 1;
-    const long long units = (long long)kv->batch * kv->n_kv_heads * pl.grid_tiles;
-    const double per_block = 1.28, fixed = 10.0;  // us: one 60-node tree over 2k tokens by 1, 2, 3, 6, 9 chunks: 38, 30, 26, 22, 23
+    const double units = (double)kv->batch * kv->n_kv_heads * pl.grid_tiles;
+    const double per_block = 1.28, fixed = 10.0;  // us
     const double partial = 2.0 * (double)total_q * tree->n_q_heads * kv->head_dim * 2.0 / 5e6;
     int best = 1;
     double best_cost = 0.0;
     const int most = num_splits > 0 ? 1 : (blocks < 64 ? blocks : 64);
     for (int s = 1; s <= most; ++s) {
-      const long long waves = (units * s + sms - 1) / sms;
-      const double cost = (double)waves * (ceil_div(blocks, s) * per_block + fixed) + (s > 1 ? partial * s + 1.0 + 0.5 * s : 0.0);
+      const double longest = ceil_div(blocks, s) * per_block + fixed;
+      double cost = longest;
+      if (units * s > sms) {
+        const double even = ceil(units * s / sms) * longest;                                          // waves of equal chunks
+        const double ragged = units * (0.75 * blocks * per_block + fixed * s) / sms + 0.5 * longest;  // of any length
+        const double sum = 0.3 * even + 0.7 * ragged;
+        if (sum > longest) cost = sum;
+      }
+      if (s > 1) cost += partial * s + 1.0 + 0.5 * s;
       if (s == 1 || cost < best_cost) {
         best = s;
         best_cost = cost;
@@ -107,12 +122,14 @@ static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree,
   // pays from about 5k keys on (32k: 67 us by 8, 29 by 32); then one wave of two CTAs per SM.
   pl.grid_tiles = ceil_div(rows, 16);
   const int groups = (int)((keys + 31) / 32) + (window > 0 ? 2 : 0) + ceil_div(tree->max_nodes, 16);
-  const long long units = (long long)kv->batch * kv->n_kv_heads * pl.grid_tiles;
+  const long long units = tiles;
   int s;
   if (num_splits > 0) {
     s = num_splits;
   } else {
     s = (int)((520 + units - 1) / units);
+    // several tiles of rows: 32 of them over 2k keys 23 / 17 / 14 / 19 us by 2 / 4 / 6 / 8 chunks, 64: 24 / 19 / 19 / 33
+    if (rows > 16 && units > 16) s = units > 32 ? 4 : 6;
     const int most = ceil_div(groups, 4);  // a group for each of the four warps
     if (s > most) s = most;
     if (s > kQuantMaxCluster) {

@@ -442,7 +442,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     auto walk = [&](int i, int group, uint32_t s_addr) {
       uint32_t x[32];
       tmem_ld32_async(s_addr, x);
-#pragma unroll 1
+#pragma unroll
       for (int q = 0; q < 2; ++q) {
         const float2 ks = *reinterpret_cast<const float2*>(s_ks + group + 2 * q);
         const float2 ls = *reinterpret_cast<const float2*>(s_lsv + group + 2 * q);
