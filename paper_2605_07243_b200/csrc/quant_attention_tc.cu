@@ -96,7 +96,7 @@ __device__ inline void warp_commit(uint32_t elected, uint64_t* bar) {
 }
 // 2^x for two values by the FMA pipe: x = n + f, |f| <= 1/2 (adding 1.5 * 2^23 rounds x to an integer, which the low bits of the sum then
 // hold), 2^f by a polynomial of degree 4 fitted for equal relative error by Remez exchange (2.6e-6), 2^n by the exponent
-// bits.  x <= 100; below -126 the result is 2^-126.
+// bits.  Below -126 the result is 2^-126; above 126 it means nothing.
 __device__ inline void exp2_by_fma(float x0, float x1, float& y0, float& y1) {
   auto both = [](float v) { return pack_f32x2(v, v); };
   const unsigned long long x = pack_f32x2(fmaxf(x0, -126.f), fmaxf(x1, -126.f));
@@ -110,6 +110,11 @@ __device__ inline void exp2_by_fma(float x0, float x1, float& y0, float& y1) {
   unpack_f32x2(t, t0, t1);
   y0 = __uint_as_float(__float_as_uint(q0) + (__float_as_uint(t0) << 23));
   y1 = __uint_as_float(__float_as_uint(q1) + (__float_as_uint(t1) << 23));
+}
+__device__ inline float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
 }
 // 32 columns without the wait
 __device__ inline void tmem_ld32_async(uint32_t taddr, uint32_t (&r)[32]) {
@@ -176,7 +181,6 @@ __device__ inline uint32_t code_tile_off(int r, int ch) {
 struct ScaleRing {
   // Eight slots: the loader writes block j's when S of block j - 3 is done, i.e. the softmax with block j - 5.
   float *ks, *lsv, *isv;   // [8 slots][8 groups of 16 keys]: K scale, log2 of the V scale, 1 / V scale
-  uint32_t* flag;          // [8 slots]: bits 0-7 the groups with a NaN scale, bits 8-15 those whose V reads as zeros
 };
 
 // Lane -> (row, 16-element chunk) when a warp moves rows of D elements, 32 / (D / 16) rows at a time.  D = 128: eight neighbouring
@@ -237,19 +241,13 @@ __device__ inline int node_exponent(const uint4 (&x)[N], int up, int least) {
   amax = __reduce_max_sync(0xffffffffu, amax);
   return min(amax < 0x80u ? 127 : max((int)(amax >> 7) - up, least), 253);
 }
-// 16 rows of the tree (group grp): K as two e4m3 terms into k1 and k2, V as fp16 into v16, the scales of both (slot 0 of the ring) and the
-// bits of bad rows.  One warp.  Out of line: its registers stay out of the main loop.
+// 16 rows of the tree (group grp), one warp: V as fp16, or K as two e4m3 terms, and their scale (slot 0 of the ring).
 template <int D>
-static __device__ __noinline__ void node_group(const bf16* k_nodes, const bf16* v_nodes, long long stride, int n, int grp, uint8_t* k1, uint8_t* k2,
-                                        uint8_t* v16, ScaleRing ring, uint32_t* s_bad) {
+__device__ inline void put_node_v(int grp, int lane, const uint4 (&x)[D / 16], uint8_t* v16, ScaleRing ring) {
   constexpr int RPI = 512 / D, NI = 16 / RPI;
-  const int lane = threadIdx.x & 31, ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
-  uint4 x[D / 16], y[D / 16];
-  load_node_rows<D>(v_nodes, stride, n, grp, lane, x);
-  load_node_rows<D>(k_nodes, stride, n, grp, lane, y);
-  const uint32_t bits = drop_bad_rows<D>(lane, x) | drop_bad_rows<D>(lane, y);
+  const int ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
   const int ev = node_exponent(x, 8, 127 - 60);  // (see v_scale_used)
-  float inv = __uint_as_float((uint32_t)(254 - ev) << 23);
+  const float inv = __uint_as_float((uint32_t)(254 - ev) << 23);
 #pragma unroll
   for (int i = 0; i < NI; ++i)
 #pragma unroll
@@ -260,8 +258,17 @@ static __device__ __noinline__ void node_group(const bf16* k_nodes, const bf16* 
       for (int c = 0; c < 4; ++c) h[c] = pack_f16(__uint_as_float(w[c] << 16) * inv, __uint_as_float(w[c] & 0xFFFF0000u) * inv);
       *reinterpret_cast<uint4*>(v16 + sw128_chunk_off(16 * grp + i * RPI + r_in, 2 * ch + k, TC_BN)) = make_uint4(h[0], h[1], h[2], h[3]);
     }
+  if (lane == 0) {
+    ring.lsv[grp] = (float)(ev - 127);
+    ring.isv[grp] = __uint_as_float((uint32_t)(254 - ev) << 23);
+  }
+}
+template <int D>
+__device__ inline void put_node_k(int grp, int lane, const uint4 (&y)[D / 16], uint8_t* k1, uint8_t* k2, ScaleRing ring) {
+  constexpr int RPI = 512 / D, NI = 16 / RPI;
+  const int ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
   const int ek = node_exponent(y, 7, 1);
-  inv = __uint_as_float((uint32_t)(254 - ek) << 23);
+  const float inv = __uint_as_float((uint32_t)(254 - ek) << 23);
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
     uint32_t hi[4], lo[4];
@@ -281,12 +288,7 @@ static __device__ __noinline__ void node_group(const bf16* k_nodes, const bf16* 
     *reinterpret_cast<uint4*>(k1 + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
     *reinterpret_cast<uint4*>(k2 + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
   }
-  if (lane == 0) {
-    ring.ks[grp] = __uint_as_float((uint32_t)ek << 23);
-    ring.lsv[grp] = (float)(ev - 127);
-    ring.isv[grp] = __uint_as_float((uint32_t)(254 - ev) << 23);
-    if (bits) atomicOr(&s_bad[grp >> 1], bits << (16 * (grp & 1)));
-  }
+  if (lane == 0) ring.ks[grp] = __uint_as_float((uint32_t)ek << 23);
 }
 
 // Scores of 32 columns whose bit is not set become -inf.
@@ -298,6 +300,51 @@ static __device__ __noinline__ void mask_scores(uint32_t addr, uint32_t word) {
     if (!((word >> e) & 1u)) x[e] = 0xff800000u;
   tmem_st32(addr, x);
   tmem_wait_st();
+}
+
+// The CTA's sequence, KV head and row tile when CTAs are handed out in order: sequences longest first, for each its heads, for each head
+// the tiles that it has (at least one).  False for the CTAs behind the last.  A grid of the longest tree's tiles for every sequence, run as
+// it is, starts CTAs without work before others with much (16 windowed trees of 5 to 33 nodes 36.3 us; so, 35.6).  batch <= SB_MAX_NODES;
+// s_len: 16-byte aligned scratch of 2 * SB_MAX_NODES ints, s_pick: two ints.
+__device__ inline bool quant_unit_of_rank(const QuantAttnParams& p, int most, int* s_len, int* s_pick, int& b, int& g, int& tile) {
+  const int B = p.kv.batch, tid = threadIdx.x;
+  int* s_tiles = s_len + SB_MAX_NODES;
+  for (int i = tid; i < SB_MAX_NODES; i += blockDim.x) {
+    int len = (int)0x80000000, n = 0;
+    if (i < B) {
+      len = p.tree.prefix_len[i];
+      n = p.tree.node_offsets[i + 1] - p.tree.node_offsets[i] - (p.q_node_begin ? p.q_node_begin[i] : 0);
+      n = min(max(ceil_div(min(max(n, 0), SB_MAX_NODES) * p.G, TC_BM), 1), most);
+    }
+    s_len[i] = len;
+    s_tiles[i] = n;
+  }
+  if (tid == 0) s_pick[0] = -1;
+  __syncthreads();
+  const int unit = blockIdx.z * gridDim.y + blockIdx.y, Hkv = p.kv.n_kv_heads;
+  for (int i = tid; i < B; i += blockDim.x) {
+    const int me = s_len[i];
+    int start = 0;
+#pragma unroll 4
+    for (int j = 0; j < B; j += 4) {
+      const int4 o = *reinterpret_cast<const int4*>(s_len + j), t = *reinterpret_cast<const int4*>(s_tiles + j);
+      start += (o.x > me || (o.x == me && j < i) ? t.x : 0) + (o.y > me || (o.y == me && j + 1 < i) ? t.y : 0) +
+               (o.z > me || (o.z == me && j + 2 < i) ? t.z : 0) + (o.w > me || (o.w == me && j + 3 < i) ? t.w : 0);
+    }
+    if (unit >= start * Hkv && unit < (start + s_tiles[i]) * Hkv) {
+      s_pick[0] = i;
+      s_pick[1] = start;
+    }
+  }
+  __syncthreads();
+  b = s_pick[0];
+  if (b >= 0) {
+    const int mine = unit - s_pick[1] * Hkv;
+    g = mine / s_tiles[b];
+    tile = mine - g * s_tiles[b];
+  }
+  __syncthreads();
+  return b >= 0;
 }
 
 template <int D>
@@ -315,7 +362,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   volatile int* s_abort = reinterpret_cast<volatile int*>(base + 3332);   // [0] a wait gave up; [1] the same for the last wait
   int* s_err = reinterpret_cast<int*>(base + 3340);
   uint32_t* s_bad = reinterpret_cast<uint32_t*>(base + 3344);        // [4]: node rows with a NaN or an infinity
-  uint32_t* s_flag = reinterpret_cast<uint32_t*>(base + 3360);       // [8 slots]: see ScaleRing
+  uint32_t* s_flag = reinterpret_cast<uint32_t*>(base + 3360);       // [8 slots]: bits 0-7 the groups with a NaN scale, bits 8-15 those whose V reads as zeros
   float* s_ks = reinterpret_cast<float*>(base + 7168);               // [8 slots][8 groups of 16 keys] K scale
   float* s_lsv = s_ks + 64;                                          // log2 of the V scale
   float* s_isv = s_lsv + 64;                                         // 1 / V scale
@@ -348,12 +395,18 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   pdl_wait();
   pdl_release();
 
+  // The tiles of a KV head are neighbours: they share its codes in L2.
   const int tiles = (int)gridDim.y / Hkv;
-  const int g = blockIdx.y / tiles, row0 = (int)(blockIdx.y % tiles) * TC_BM;   // the tiles of a KV head are neighbours: they share its codes in L2
-  const int b = p.sort_seqs ? quant_sequence_of_rank(p, blockIdx.z, reinterpret_cast<int*>(s_anc), s_parent) : (int)blockIdx.z;
+  int b = blockIdx.z, g = blockIdx.y / tiles, tile = blockIdx.y % tiles;
+  if (p.sort_seqs && !quant_unit_of_rank(p, tiles, reinterpret_cast<int*>(s_anc), s_parent, b, g, tile)) {
+    if (warp == QT_MMA_WARP)
+      asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(*s_tmem), "r"(QT_TMEM_COLS));
+    return;
+  }
+  const int row0 = tile * TC_BM;
   const QuantSeq si = load_quant_seq(p, b);
   const int rows_total = si.nq * G;
-  const bool designated = split == 0 && blockIdx.y == 0;
+  const bool designated = split == 0 && g == 0 && tile == 0;
   if (!si.can_write || row0 >= rows_total) {
     if (designated) {
       const bool pages_ok = si.err ? true : quant_pages_in_pool(p.kv, b, si.P, whole_cta());
@@ -383,12 +436,15 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   bool ok = true, compute = false;
 
   if (warp < QT_SOFTMAX / 32) {
-    if (tree_blocks) {
-      const ScaleRing ring = {s_ks, s_lsv, s_isv, s_flag};
-      const long long first = (long long)si.node_base * p.node_stride + g * D;
-      node_group<D>(p.k_nodes + first, p.v_nodes + first, p.node_stride, si.n, warp, sK, sK2, sV, ring, s_bad);
-    }
-    // ---- Q: 16-byte pieces, D / 8 lanes to a row, all loads in flight at once -----------------------------------------
+    // All global loads first.  Nodes: warp w takes V (w even) or K (odd) of groups w / 2 and 4 + w / 2 of 16 nodes.
+    const int groups = tree_blocks ? (si.n + 15) >> 4 : 0;
+    uint4 xn[2][D / 16];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (4 * h + (warp >> 1) < groups)
+        load_node_rows<D>((warp & 1 ? p.k_nodes : p.v_nodes) + (long long)si.node_base * p.node_stride + g * D, p.node_stride, si.n,
+                          4 * h + (warp >> 1), lane, xn[h]);
+    // Q: 16-byte pieces, D / 8 lanes to a row
     constexpr int LPR = D / 8, RPP = QT_SOFTMAX / LPR, NQ = TC_BM / RPP;
     const int ch = tid % LPR;
     uint4 xq[NQ];
@@ -399,6 +455,24 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       xq[i] = make_uint4(0, 0, 0, 0);
       if (R < rows_total && SB_CHECKED_ACCESS(si.q_off + nl, p.total_q, &p.status[b]))
         xq[i] = __ldg(reinterpret_cast<const uint4*>(p.q + (long long)(si.q_off + nl) * p.q_stride + (g * G + hh) * D + ch * 8));
+    }
+    const ScaleRing ring = {s_ks, s_lsv, s_isv};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int grp = 4 * h + (warp >> 1);
+      if (grp >= groups) continue;
+      const uint32_t bits = drop_bad_rows<D>(lane, xn[h]);
+      if (bits && lane == 0) atomicOr(&s_bad[grp >> 1], bits << (16 * (grp & 1)));
+      if (warp & 1) put_node_k<D>(grp, lane, xn[h], sK, sK2, ring);
+      else put_node_v<D>(grp, lane, xn[h], sV, ring);
+    }
+    if (tree_blocks) {  // groups without nodes: K may be anything (masked), V has to be finite
+      for (int i = groups * 2 * D + tid; i < TC_BN * D / 8; i += QT_SOFTMAX)
+        *reinterpret_cast<uint4*>(sV + sw128_chunk_off(i / (D / 8), i % (D / 8), TC_BN)) = make_uint4(0, 0, 0, 0);
+      if (tid >= groups && tid < 8) {
+        s_ks[tid] = s_isv[tid] = 1.f;
+        s_lsv[tid] = 0.f;
+      }
     }
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
@@ -448,7 +522,8 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
         const float2 ls = *reinterpret_cast<const float2*>(s_lsv + group + 2 * q);
         const float2 is = *reinterpret_cast<const float2*>(s_isv + group + 2 * q);
         // exponents relative to the present reference
-        const float f0 = qs * ks.x, f1 = qs * ks.y, c0 = ls.x - ref, c1 = ls.y - ref;
+        // (a factor that underflows would turn the -inf of an invisible key into NaN; a NaN factor stays)
+        const float f0 = max_nan(qs * ks.x, 1.17549435e-38f), f1 = max_nan(qs * ks.y, 1.17549435e-38f), c0 = ls.x - ref, c1 = ls.y - ref;
         const unsigned long long mul[2] = {pack_f32x2(f0, f0), pack_f32x2(f1, f1)}, add[2] = {pack_f32x2(c0, c0), pack_f32x2(c1, c1)};
         tmem_wait_ld(x);
         float d[32];
@@ -481,6 +556,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
             }
             rescale_row<D>(i > 0 ? tmem_o + t_mine * D + lane_base : 0xffffffffu, s_addr, q, factor);
           }
+          float most = 0.f;  // of the exponents whose exponential would not show by its size how large they are
           unsigned long long sum2[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
 #pragma unroll
           for (int e = 0; e < 32; e += 2) {
@@ -488,6 +564,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
             float p0, p1;
             if ((e & 7) == 6) {
               exp2_by_fma(d[e], d[e + 1], p0, p1);
+              most = max3(most, d[e], d[e + 1]);
             } else {
               p0 = fast_exp2(d[e]);
               p1 = fast_exp2(d[e + 1]);
@@ -500,7 +577,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
           unpack_f32x2(sum2[1], b0, b1);
           a0 += a1;
           b0 += b1;
-          raise = a0 + b0 > kQuantLimit;
+          raise = a0 + b0 > kQuantLimit || most > 14.f;
           if (!__any_sync(0xffffffffu, raise)) break;
         }
         l_run = fmaf(b0, is.y, fmaf(a0, is.x, l_run));
@@ -528,7 +605,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
           if (is_tree) {
             const int w0 = (k0 >> 5) + q;    // k0: first node of the step
             word = node >= 0 ? s_anc[4 * node + w0] : 0u;
-            if (p.window > 0) {
+            if (p.window > 0 && p.window < si.n) {  // (a node's ancestors lie less than n positions back)
               for (uint32_t w = word; w; w &= w - 1) {
                 const int bit = __ffs(w) - 1, kp = si.P + s_depth[32 * w0 + bit];
                 if (!(kp < p.sinks || pos - kp < p.window)) word &= ~(1u << bit);
