@@ -169,6 +169,8 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const sb_page
   pdl_release();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, ps = pool.page_size;
   ReserveWs ws(wsp, pool, n);
+  __shared__ unsigned long long s_wants;
+  if (tid == 0) s_wants = 0;
   for (int i = tid; i < pool.num_pages; i += PG_THREADS) {
     ws.count[i] = 0;
     ws.first_of[i] = 0x7fffffff;
@@ -220,18 +222,20 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const sb_page
     if (lane == 0) {
       ws.want[i] = wants;
       ws.copies[i] = copies;
+      atomicAdd(&s_wants, (unsigned long long)wants);
     }
   }
   __syncthreads();
-  // ranks in list order (a sum beyond the pool's size only has to stay beyond it)
-  int wants_total = 0, copies_total = 0;
+  // ranks in list order; what the pool cannot hold at all is refused below, without sums that might leave 32 bits
+  const bool too_many = s_wants > (unsigned long long)pool.num_pages;
+  int wants_total = too_many ? 1 : 0, copies_total = 0;
   for (int i0 = 0; i0 < n; i0 += PG_THREADS) {
     const int i = i0 + tid;
     int t;
     const int w = i < n ? ws.want[i] : 0;
-    const int wx = block_exclusive(w, s_scan, &t);
+    const int wx = block_exclusive(too_many ? 0 : w, s_scan, &t);
     if (i < n) ws.want[i] = wants_total + wx;
-    wants_total = min(wants_total + t, 0x3fffffff);
+    wants_total += t;
     const int c = i < n ? ws.copies[i] : 0;
     const int cx = block_exclusive(c, s_scan, &t);
     if (i < n) ws.copies[i] = copies_total + cx;
@@ -241,7 +245,7 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const sb_page
   }
   // the lowest free pages, ascending
   int found = 0;
-  for (int p0 = 0; p0 < pool.num_pages && found < wants_total; p0 += PG_THREADS) {
+  for (int p0 = 0; p0 < pool.num_pages && found < wants_total && !too_many; p0 += PG_THREADS) {
     const int p = p0 + tid;
     const int is_free = p < pool.num_pages && pool.refs[p] == 0 ? 1 : 0;
     int t;
@@ -562,7 +566,7 @@ extern "C" sb_status sb_pages_copy(const sb_page_array* arrays, int32_t n_arrays
     if (!a.base || a.page_bytes < 4 || a.page_bytes % 4 != 0 || a.layer_stride < 0 || a.layer_stride % 4 != 0 ||
         (reinterpret_cast<uintptr_t>(a.base) & 3))
       return SB_ERR_INVALID_ARG;
-    if (n_layers > 1 && a.layer_stride < a.page_bytes * num_pages) return SB_ERR_INVALID_ARG;  // layers would overlap
+    if (n_layers > 1 && a.layer_stride / num_pages < a.page_bytes) return SB_ERR_INVALID_ARG;  // layers would overlap
     arr.a[i] = a;
     pieces += (a.page_bytes + PC_PIECE - 1) / PC_PIECE;
     if (pieces > (1 << 30)) return SB_ERR_UNSUPPORTED;

@@ -294,3 +294,31 @@ def test_the_checked_build_finds_no_access_out_of_bounds():
         sb.sb_pages_compact(gpu, copies)
         torch.cuda.synchronize()
         assert sb.sb_checked_violations() == 0
+
+
+def test_pages_wishes_beyond_32_bits_are_refused():
+    """1040 empty slots that ask for 2^21 pages each of a pool of ten."""
+    slots, most = 1040, 1 << 21
+    pool = sb.PagePool(16, torch.empty(slots, most, dtype=torch.int32, device="cuda"), torch.zeros(slots, dtype=torch.int32, device="cuda"),
+                       torch.zeros(10, dtype=torch.int32, device="cuda"))
+    copies = sb.PageCopies.empty(slots)
+    want = [most * 16] * slots
+    want[7] = 0
+    status = sb.sb_pages_reserve(pool, i32(range(slots)), i32([0] * slots), i32(want), copies)
+    assert status.cpu().tolist() == [7 if i != 7 else 0 for i in range(slots)]
+    assert not pool.held.any() and not pool.refs.any() and copies.count.item() == 0
+
+
+def test_rows_behind_the_last_sequence_stay_as_they_are():
+    for P, N, H in (([40, 0], [1, 2], 2), ([300, 100], [90, 33], 8)):
+        cache, parents, q, k, v = make(70, P, N, H=H, G=2)
+        total = q.shape[0]
+        want, wlse = check(cache, P, parents, q, k, v)
+        more = torch.cat([q, q[:5]]).cuda()
+        out, lse = torch.full_like(more, 3.0), torch.full(more.shape[:2], 3.0, device="cuda")
+        for num_splits in (0, 11):
+            sb.sb_tree_attention_quant(cache.gpu(sb), tree_of(P, parents, 2 * H), more, k.cuda(), v.cuda(), out=out, lse=lse, num_splits=num_splits,
+                                       q_offsets=i32([0, N[0]]))
+            assert (out[total:] == 3.0).all() and (lse[total:] == 3.0).all()
+            if num_splits == 0:
+                assert torch.equal(out[:total], want) and torch.equal(lse[:total], wlse)
