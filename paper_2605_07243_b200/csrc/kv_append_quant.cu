@@ -9,10 +9,12 @@
 //
 // Bound by memory for prompts: 2 bytes read and 1 written per element.  A unit of work is one (block, head, K or V): the maximum
 // needs the whole block before the first code can be written, so the new rows stay in registers between the two
-// steps, 64 elements a thread.  Prompts: one CTA of 2 * scale_block threads per unit, so that many small CTAs hide one
-// another's chain of dependent loads (lengths, rows and page ids, old scale).  Up to 16 rows (a verified step): one warp per
-// unit, eight to a CTA; there the chain is all there is, and a commit has thousands of units of a few hundred bytes.
-// Row loads go out before the page ids are looked at.  Elements past the new rows are never touched.
+// steps, 64 elements a thread.  Prompts: 2 * scale_block threads per unit, and many units on an SM hide one
+// another's chain of dependent loads (lengths, rows and page ids, old scale).  Four prompts of 2000 to 8192 tokens: 31 us, 4.0 TB/s;
+// without the stores 21 us, the launch alone 9.  Up to 16 rows (a verified step): one warp per unit; there the chain is all there
+// is, and a commit has thousands of units of a few hundred bytes: 16 sequences, 32 layers 11.4 us, of which the launch and the chain up
+// to the rows take 5.  (One warp for both blocks that a path may touch, instead of a warp each of which the second mostly finds
+// nothing to do: 12.6.)  Row loads go out before the page ids are looked at.  Elements past the new rows are never touched.
 #include "quant_common.cuh"
 
 namespace sb {
@@ -66,26 +68,37 @@ static __device__ __noinline__ uint2 rescaled(uint2 v, float old, float s) {
   return make_uint2(out[0], out[1]);
 }
 
-// UT threads to a unit: a whole CTA, or one warp of a CTA of eight (UT = 32).
+// UT threads to a unit.  A CTA has 256 threads whatever the unit: 20,000 prompt tokens in blocks of 64 are 5000 units of 128 threads, and
+// starting a CTA for each took 9 of 33 us (31 so; 384 and 512 threads 35.6 and 33).
+constexpr int kAppendThreads = 256;
 template <int D, int UT>
-__global__ void __launch_bounds__(UT == 32 ? 256 : UT, UT == 32 ? 4 : 1152 / UT) kv_append_quant_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(kAppendThreads, 4) kv_append_quant_kernel(const AppendParams p) {
   constexpr int LPR = D / 8;              // lanes per row: 8 elements (16 bytes of bf16) each
   constexpr int RPP = UT / LPR;           // rows per pass
   constexpr int ROWS = UT == 32 ? 16 : UT / 2;
   constexpr int PASSES = ROWS / RPP;
-  constexpr int UNITS = UT == 32 ? 8 : 1;
+  constexpr int UNITS = kAppendThreads / UT;
   __shared__ int s_path[UNITS][SB_MAX_DEPTH + 1];
-  __shared__ uint32_t s_max[UT == 32 ? 1 : UT / 32];
-  auto sync = []() {
-    if (UT == 32) __syncwarp();
-    else __syncthreads();
-  };
-  // the same value in every thread of the unit
-  auto any = [](bool v) { return UT == 32 ? __any_sync(0xffffffffu, v) != 0 : __syncthreads_or(v) != 0; };
-  pdl_wait();
-  pdl_release();
+  __shared__ uint32_t s_max[UNITS][UT / 32];
   const int H = p.kv.n_kv_heads, sb = p.kv.scale_block;
   const int tid = threadIdx.x % UT, slot = threadIdx.x / UT;
+  auto sync = [slot]() {
+    if (UT == 32) __syncwarp();
+    else asm volatile("barrier.sync %0, %1;" ::"r"(slot + 1), "n"(UT) : "memory");
+  };
+  // the same value in every thread of the unit
+  auto any = [slot](bool v) {
+    if (UT == 32) return __any_sync(0xffffffffu, v) != 0;
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
+        : "=r"(r)
+        : "r"((uint32_t)v), "r"(slot + 1), "n"(UT)
+        : "memory");
+    return r != 0;
+  };
+  pdl_wait();
+  pdl_release();
   const int b = blockIdx.y, layer = blockIdx.z;
   const int unit = blockIdx.x * UNITS + slot, which = unit & 1, g = (unit >> 1) % H, nth = (unit >> 1) / H;
   const int start = p.len[b];
@@ -174,11 +187,11 @@ __global__ void __launch_bounds__(UT == 32 ? 256 : UT, UT == 32 ? 4 : 1152 / UT)
     }
     m = __reduce_max_sync(0xffffffffu, max(m & 0xFFFFu, m >> 16));
     if (UT > 32) {
-      __syncthreads();
-      if ((tid & 31) == 0) s_max[tid >> 5] = m;
-      __syncthreads();
+      sync();
+      if ((tid & 31) == 0) s_max[slot][tid >> 5] = m;
+      sync();
 #pragma unroll
-      for (int i = 0; i < UT / 32; ++i) m = max(m, s_max[i]);
+      for (int i = 0; i < UT / 32; ++i) m = max(m, s_max[slot][i]);
     }
     return m;
   };
@@ -266,12 +279,13 @@ extern "C" sb_status sb_kv_append_quant(const sb_quant_cache* kv, const void* k_
   const long long units = (((long long)most + sb - 2) / sb + 1) * 2 * kv->n_kv_heads;
   if (units > 0x7fffffffLL) return SB_ERR_UNSUPPORTED;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  auto launch = [&](auto kernel, int threads, int units_per_cta) {
-    return launch_dependent(kernel, dim3((unsigned)((units + units_per_cta - 1) / units_per_cta), kv->batch, kv->n_layers), dim3(threads), cs, p);
+  auto launch = [&](auto kernel, int unit_threads) {
+    const int per_cta = kAppendThreads / unit_threads;
+    return launch_dependent(kernel, dim3((unsigned)((units + per_cta - 1) / per_cta), kv->batch, kv->n_layers), dim3(kAppendThreads), cs, p);
   };
   const bool d64 = kv->head_dim == 64;
-  if (most <= 16 || sb == 16) return d64 ? launch(kv_append_quant_kernel<64, 32>, 256, 8) : launch(kv_append_quant_kernel<128, 32>, 256, 8);
-  if (sb == 32) return d64 ? launch(kv_append_quant_kernel<64, 64>, 64, 1) : launch(kv_append_quant_kernel<128, 64>, 64, 1);
-  if (sb == 64) return d64 ? launch(kv_append_quant_kernel<64, 128>, 128, 1) : launch(kv_append_quant_kernel<128, 128>, 128, 1);
-  return d64 ? launch(kv_append_quant_kernel<64, 256>, 256, 1) : launch(kv_append_quant_kernel<128, 256>, 256, 1);
+  if (most <= 16 || sb == 16) return d64 ? launch(kv_append_quant_kernel<64, 32>, 32) : launch(kv_append_quant_kernel<128, 32>, 32);
+  if (sb == 32) return d64 ? launch(kv_append_quant_kernel<64, 64>, 64) : launch(kv_append_quant_kernel<128, 64>, 64);
+  if (sb == 64) return d64 ? launch(kv_append_quant_kernel<64, 128>, 128) : launch(kv_append_quant_kernel<128, 128>, 128);
+  return d64 ? launch(kv_append_quant_kernel<64, 256>, 256) : launch(kv_append_quant_kernel<128, 256>, 256);
 }
