@@ -4,11 +4,11 @@
 
 namespace sb {
 
-// Log-sum-exp merge of the chunks' partials, 16 bytes of a row per lane.  PB16: bf16 partials (tcgen05 kernel), else fp32.
+// Log-sum-exp merge of the chunks' partials, 16 bytes of a row per lane.  P16: fp16 partials with exponents (tcgen05 kernel), else fp32.
 // A NaN partial makes the row NaN.
-template <int D, bool PB16>
+template <int D, bool P16>
 __global__ void __launch_bounds__(256) quant_merge_kernel(const QuantAttnParams p) {
-  constexpr int EPL = PB16 ? 8 : 4, LPR = D / EPL, RPW = 32 / LPR;
+  constexpr int EPL = P16 ? 8 : 4, LPR = D / EPL, RPW = 32 / LPR;
   pdl_wait();
   pdl_release();
   const int b = blockIdx.y;
@@ -28,16 +28,18 @@ __global__ void __launch_bounds__(256) quant_merge_kernel(const QuantAttnParams 
 #pragma unroll 4
   for (int s = 0; s < p.outer; ++s) {
     const float lse2 = p.part_lse[s * rows_all + grow];
-    const uint4 raw = *reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p.part_o) +
-                                                      ((s * rows_all + grow) * D + col * EPL) * (PB16 ? 2 : 4));
-    const float w = lse2 == -INFINITY ? 0.f : fast_exp2(lse2 - M);
+    const char* row = reinterpret_cast<const char*>(p.part_o) + (s * rows_all + grow) * (P16 ? kPartRow<D> : D * 4);
+    const uint4 raw = *reinterpret_cast<const uint4*>(row + col * 16);
+    float w = lse2 == -INFINITY ? 0.f : fast_exp2(lse2 - M);
     sum += w;
+    if (P16) w *= __uint_as_float((uint32_t)(*reinterpret_cast<const uint8_t*>(row + D * 2 + col) - 14) << 23);
     const uint32_t u[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      if (PB16) {
-        acc[(2 * e) % EPL] = fmaf(w, __uint_as_float(u[e] << 16), acc[(2 * e) % EPL]);
-        acc[(2 * e + 1) % EPL] = fmaf(w, __uint_as_float(u[e] & 0xFFFF0000u), acc[(2 * e + 1) % EPL]);
+      if (P16) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&u[e]));
+        acc[(2 * e) % EPL] = fmaf(w, f.x, acc[(2 * e) % EPL]);
+        acc[(2 * e + 1) % EPL] = fmaf(w, f.y, acc[(2 * e + 1) % EPL]);
       } else {
         acc[e] = fmaf(w, __uint_as_float(u[e]), acc[e]);
       }
@@ -86,7 +88,7 @@ static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree,
   if (pl.tc) {
     // A CTA costs its key blocks plus a fixed start and end.  CTAs start longest first on whichever SM is free: equal ones run in waves,
     // ragged ones (three quarters of the longest, taken on average) end about half a chunk unevenly; the estimate lies between the two.
-    // Every chunk beyond the first writes and re-reads bf16 partials of all rows, and the merge is one more kernel.  us by 1 / 2 / 3 / 4 /
+    // Every chunk beyond the first writes and re-reads fp16 partials of all rows, and the merge is one more kernel.  us by 1 / 2 / 3 / 4 /
     // 6 chunks: one 60-node tree over 2k keys 38 / 30 / 26 / 24 / 22; 8-node trees over ragged 8k prefixes, 4 of them 89 / 54 / 42 / 37 /
     // 40, 16: 91 / 74 / 82 / 89 / 104, 64: 209 / 244 / 273 / 299 / 355; four full trees, 64 heads, over 32k keys 695 / 724 / 725 / 690 / 772.
     pl.grid_tiles = ceil_div(rows, 128);

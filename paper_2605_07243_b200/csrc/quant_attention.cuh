@@ -28,7 +28,7 @@ struct QuantAttnParams {
   int window, sinks;
   int num_splits;   // chunks of the key list per (sequence, KV head, row tile) = cluster size * outer
   int outer;        // clusters; > 1 needs the merge kernel
-  float* part_o;    // [outer][total_q * Hq][D] normalised partial outputs
+  float* part_o;    // [outer][total_q * Hq][D] normalised partial outputs (tcgen05 kernel: rows of kPartRow bytes)
   float* part_lse;  // [outer][total_q * Hq]    base-2 log-sum-exp of each
   int* status;
   int G;
@@ -152,6 +152,10 @@ inline sb_status make_code_maps(const QuantAttnParams& p, int most, CUtensorMap*
   return SB_OK;
 }
 
+// Bytes of a partial row of the tcgen05 kernel: fp16 values, and the exponent of every eight of them (16 bytes; value = fp16 *
+// 2^(exponent - 141)).
+template <int D>
+constexpr int kPartRow = 2 * D + 16;
 constexpr int kQuantMaxCluster = 8;
 sb_status launch_quant_rows(const QuantAttnParams& p, dim3 grid, int cluster, cudaStream_t cs);
 sb_status launch_quant_tc(const QuantAttnParams& p, dim3 grid, cudaStream_t cs);
