@@ -521,9 +521,9 @@ typedef struct sb_quant_tree {
  *   q_node_begin, q_offsets and status as for sb_tree_attention.  q_stride and node_stride are multiples of 8,
  *   q, k_nodes, v_nodes and out 16-byte aligned.  `layer` picks one of the cache's layers.
  *   A node row of K or V that holds a NaN or an infinity makes the outputs of the nodes that see it NaN and
- *   changes no other node's.  Scores, softmax and outputs are accumulated in fp32; Q (scaled by a power of two
- *   per row), the codes and the probabilities enter the products as fp16 (node rows: fp16 with a power of two
- *   per 16 nodes, or bf16).
+ *   changes no other node's.  Scores, softmax and outputs are accumulated in fp32.  The codes enter the products as
+ *   they are; Q, scaled by a power of two per row, as fp16 or as two e4m3 terms; node rows as bf16, or scaled by a
+ *   power of two per 16 nodes (K as two e4m3 terms, V as fp16); the probabilities as fp16 (of node rows: fp16 or bf16).
  *   workspace: sb_tree_attention_quant_workspace_bytes(...) bytes, 256-byte aligned, no initialisation; calls
  *   that may overlap on the GPU need distinct workspaces.
  */
