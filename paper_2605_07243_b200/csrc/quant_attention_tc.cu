@@ -184,10 +184,10 @@ struct ScaleRing {
 };
 
 // Lane -> (row, 16-element chunk) when a warp moves rows of D elements, 32 / (D / 16) rows at a time.  D = 128: eight neighbouring
-// lanes hold four chunks of two rows, not eight of one row: the two fp16 column halves of a row lie in the same banks, two
-// neighbouring rows in different ones.
+// lanes hold four chunks of one row and the other four of the next: 16-byte codes that lie in different banks, and so do the fp16 halves
+// that they become (a row's two fp16 column halves share their banks, two neighbouring rows do not).
 template <int D>
-__device__ inline int lane_chunk(int lane) { return D == 128 ? (lane & 3) | ((lane >> 1) & 4) : lane & 3; }
+__device__ inline int lane_chunk(int lane) { return D == 128 ? (lane & 3) | (((lane ^ (lane >> 1)) & 4)) : lane & 3; }
 template <int D>
 __device__ inline int lane_row(int lane) { return D == 128 ? ((lane >> 2) & 1) | ((lane >> 3) & 2) : lane >> 2; }
 
