@@ -38,7 +38,7 @@ constexpr int QT_CVT_WARP = 10;       // warps 10, 11: V codes -> fp16
 constexpr int QT_THREADS = 384;       // 12 warps leave 168 registers a thread
 constexpr int QT_TMEM_COLS = 512;
 constexpr int QT_SMALL = 8192;
-constexpr float kQuantLimit = 8192.f; // sum of 32 probabilities relative to the reference beyond which it is raised
+constexpr float kQuantLimit = 8192.f; // sum of a step's 64 probabilities relative to the reference beyond which it is raised
 
 enum QtBar { QB_P_FULL0, QB_P_FULL1,                                                          // 8 arrivals: the softmax warps
              QB_V_FULL0, QB_V_FULL1, QB_VR_EMPTY0, QB_VR_EMPTY1, QB_VR_EMPTY2,                // 2: the converter warps
@@ -138,31 +138,16 @@ __device__ inline void tmem_wait_ld(uint32_t (&r)[32]) {
                : "memory");
 }
 
-// Rescales a row in tensor memory: its accumulator (unless there is none yet) and the quarters of P already written
-// for the present block.  Rare, and out of line: its registers and code stay out of the main loop.
+// Rescales a row's accumulator in tensor memory.  Rare, and out of line: its registers and code stay out of the main loop.
 template <int D>
-static __device__ __noinline__ void rescale_row(uint32_t o_addr, uint32_t p_addr, int quarters, float factor) {
-  tmem_wait_st();  // what is read back was written by this thread
-  if (o_addr != 0xffffffffu) {
+static __device__ __noinline__ void rescale_row(uint32_t o_addr, float factor) {
 #pragma unroll 1
-    for (int c = 0; c < D / 16; ++c) {
-      uint32_t r[16];
-      tmem_ld16(o_addr + c * 16, r);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * factor);
-      tmem_st16(o_addr + c * 16, r);
-    }
-  }
-#pragma unroll 1
-  for (int c = 0; c < quarters; ++c) {
+  for (int c = 0; c < D / 16; ++c) {
     uint32_t r[16];
-    tmem_ld16(p_addr + 16 * c, r);
+    tmem_ld16(o_addr + c * 16, r);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&r[i]));
-      r[i] = pack_f16(f.x * factor, f.y * factor);
-    }
-    tmem_st16(p_addr + 16 * c, r);
+    for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(__uint_as_float(r[i]) * factor);
+    tmem_st16(o_addr + c * 16, r);
   }
   tmem_wait_st();
 }
@@ -511,78 +496,92 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     const float qs = s_qs[row];
     bool poison = false;
 
-    // One step's 64 scores of this row -> probabilities, 32 columns at a time, the next 32 in flight.  (Rolled: unrolled twice, the
-    // kernel outgrows the instruction caches.)
+    // One step's 64 scores of this row -> probabilities.  The two halves have no branch between them, so that one fills the
+    // gaps of the other (a check of the reference after each half: 16 trees 148 us, long trees 686; one check: 136 and 645).
     auto walk = [&](int i, int group, uint32_t s_addr) {
-      uint32_t x[32];
-      tmem_ld32_async(s_addr, x);
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const float2 ks = *reinterpret_cast<const float2*>(s_ks + group + 2 * q);
-        const float2 ls = *reinterpret_cast<const float2*>(s_lsv + group + 2 * q);
-        const float2 is = *reinterpret_cast<const float2*>(s_isv + group + 2 * q);
-        // exponents relative to the present reference
-        // (a factor that underflows would turn the -inf of an invisible key into NaN; a NaN factor stays)
-        const float f0 = max_nan(qs * ks.x, 1.17549435e-38f), f1 = max_nan(qs * ks.y, 1.17549435e-38f), c0 = ls.x - ref, c1 = ls.y - ref;
-        const unsigned long long mul[2] = {pack_f32x2(f0, f0), pack_f32x2(f1, f1)}, add[2] = {pack_f32x2(c0, c0), pack_f32x2(c1, c1)};
-        tmem_wait_ld(x);
-        float d[32];
+      const float4 ks = *reinterpret_cast<const float4*>(s_ks + group), ls = *reinterpret_cast<const float4*>(s_lsv + group);
+      const float4 is = *reinterpret_cast<const float4*>(s_isv + group);
+      // exponents relative to the present reference
+      // (a factor that underflows would turn the -inf of an invisible key into NaN; a NaN factor stays)
+      const float f[4] = {max_nan(qs * ks.x, 1.17549435e-38f), max_nan(qs * ks.y, 1.17549435e-38f), max_nan(qs * ks.z, 1.17549435e-38f),
+                          max_nan(qs * ks.w, 1.17549435e-38f)};
+      const float c[4] = {ls.x - ref, ls.y - ref, ls.z - ref, ls.w - ref};
+      const float inv_v[4] = {is.x, is.y, is.z, is.w};
+      float d[64], part[4], most = 0.f;  // most: of the exponents whose exponential would not show by its size how large they are
+      uint32_t pk[2][16];
+      auto exponents = [&](int h, const uint32_t (&x)[32]) {
 #pragma unroll
         for (int e = 0; e < 32; e += 2)
-          unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), mul[e >> 4], add[e >> 4]), d[e], d[e + 1]);
-        if (q == 0) tmem_ld32_async(s_addr + 32, x);
-        // The reference stays while no exponent is far above it.  That shows in the sum, which is needed anyway: a sum
-        // beyond 2^13 (or infinite) means an exponent above 8, and the 32 columns are done again with a new reference.
-        uint32_t pk[16];
-        float a0, b0;
-        bool raise = !seen_any;
-        while (true) {
-          if (__any_sync(0xffffffffu, raise)) {
-            float top = -INFINITY;
+          unpack_f32x2(fma_f32x2(pack_f32x2(__uint_as_float(x[e]), __uint_as_float(x[e + 1])), pack_f32x2(f[2 * h + (e >> 4)], f[2 * h + (e >> 4)]),
+                                 pack_f32x2(c[2 * h + (e >> 4)], c[2 * h + (e >> 4)])), d[32 * h + e], d[32 * h + e + 1]);
+      };
+      auto probabilities = [&](int h) {
+        unsigned long long sum2[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
 #pragma unroll
-            for (int e = 0; e < 32; e += 2) top = max3(top, d[e], d[e + 1]);
-            const float delta = raise && top > -INFINITY ? top : 0.f;
-            const float factor = seen_any ? fast_exp2(-delta) : 1.f;  // nothing accumulated yet: nothing to scale
-            seen_any |= raise && top > -INFINITY;
-#pragma unroll
-            for (int e = 0; e < 32; ++e) d[e] -= delta;
-            ref += delta;
-            l_run *= factor;
-            // the accumulator holds the steps before this one: the last of them may still be under way
-            if (i > 0) {
-              if (ok) ok = mbar_wait(&s_bar[QB_PV], (i - 1) & 1, s_abort);
-              __syncwarp();
-              tc_fence_after();
-            }
-            rescale_row<D>(i > 0 ? tmem_o + t_mine * D + lane_base : 0xffffffffu, s_addr, q, factor);
+        for (int e = 0; e < 32; e += 2) {
+          // some exponentials go to the FMA pipe: the other pipe does 16 a clock (of 64 columns 4 / 8 / 12 / 16: 134 / 136 / 136 / 138
+          // us on 16 trees, 644 / 645 / 648 / 658 on long ones)
+          float p0, p1;
+          const float d0 = d[32 * h + e], d1 = d[32 * h + e + 1];
+          if ((e & 15) == 14) {
+            exp2_by_fma(d0, d1, p0, p1);
+            most = max3(most, d0, d1);
+          } else {
+            p0 = fast_exp2(d0);
+            p1 = fast_exp2(d1);
           }
-          float most = 0.f;  // of the exponents whose exponential would not show by its size how large they are
-          unsigned long long sum2[2] = {pack_f32x2(0.f, 0.f), pack_f32x2(0.f, 0.f)};
-#pragma unroll
-          for (int e = 0; e < 32; e += 2) {
-            // a quarter of the exponentials goes to the FMA pipe: the other pipe's 16 a clock would bound the kernel
-            float p0, p1;
-            if ((e & 7) == 6) {
-              exp2_by_fma(d[e], d[e + 1], p0, p1);
-              most = max3(most, d[e], d[e + 1]);
-            } else {
-              p0 = fast_exp2(d[e]);
-              p1 = fast_exp2(d[e + 1]);
-            }
-            sum2[e >> 4] = add_f32x2(sum2[e >> 4], pack_f32x2(p0, p1));
-            pk[e >> 1] = pack_f16(p0, p1);
-          }
-          float a1, b1;
-          unpack_f32x2(sum2[0], a0, a1);
-          unpack_f32x2(sum2[1], b0, b1);
-          a0 += a1;
-          b0 += b1;
-          raise = a0 + b0 > kQuantLimit || most > 14.f;
-          if (!__any_sync(0xffffffffu, raise)) break;
+          sum2[e >> 4] = add_f32x2(sum2[e >> 4], pack_f32x2(p0, p1));
+          pk[h][e >> 1] = pack_f16(p0, p1);
         }
-        l_run = fmaf(b0, is.y, fmaf(a0, is.x, l_run));
-        tmem_st16(s_addr + 16 * q, pk);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          float u, v;
+          unpack_f32x2(sum2[k], u, v);
+          part[2 * h + k] = u + v;
+        }
+      };
+      {
+        uint32_t x0[32], x1[32];
+        tmem_ld32_async(s_addr, x0);
+        tmem_wait_ld(x0);
+        tmem_ld32_async(s_addr + 32, x1);
+        exponents(0, x0);
+        tmem_wait_ld(x1);
+        exponents(1, x1);
       }
+      // The reference stays while no exponent is far above it.  That shows in the sums, which are needed anyway: a sum
+      // beyond 2^13 (or infinite) means an exponent above 7, and the step is done again with a new reference.
+      bool raise = !seen_any;
+      while (true) {
+        if (__any_sync(0xffffffffu, raise)) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 64; e += 2) top = max3(top, d[e], d[e + 1]);
+          const float delta = raise && top > -INFINITY ? top : 0.f;
+          const float factor = seen_any ? fast_exp2(-delta) : 1.f;  // nothing accumulated yet: nothing to scale
+          seen_any |= raise && top > -INFINITY;
+#pragma unroll
+          for (int e = 0; e < 64; ++e) d[e] -= delta;
+          ref += delta;
+          l_run *= factor;
+          // the accumulator holds the steps before this one: the last of them may still be under way
+          if (i > 0) {
+            if (ok) ok = mbar_wait(&s_bar[QB_PV], (i - 1) & 1, s_abort);
+            __syncwarp();
+            tc_fence_after();
+            rescale_row<D>(tmem_o + t_mine * D + lane_base, factor);
+          }
+        }
+        most = 0.f;
+        probabilities(0);
+        probabilities(1);
+        raise = (part[0] + part[1]) + (part[2] + part[3]) > kQuantLimit || most > 14.f;
+        if (!__any_sync(0xffffffffu, raise)) break;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) l_run = fmaf(part[k], inv_v[k], l_run);
+      tmem_st16(s_addr, pk[0]);
+      tmem_st16(s_addr + 16, pk[1]);
     };
     // A wait that gives up leaves `ok` false; the loop still runs to its end, so that every barrier gets its arrivals.
     for (int i = 0; i < nb; ++i) {
