@@ -61,6 +61,8 @@ __device__ inline uint32_t pack_f16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+// Two bf16 values times a factor, as fp16.
+__device__ inline uint32_t scaled_f16(uint32_t w, float f) { return pack_f16(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xFFFF0000u) * f); }
 // kind::f8f6f4, e4m3 A and B, both K-major: the same bits with other meanings of the type fields (0 = e4m3)
 __device__ inline uint32_t tc_idesc_e4m3(int M, int N) { return (1u << 4) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24); }
 // One lane of the (converged) warp.
@@ -240,7 +242,7 @@ __device__ inline void put_node_v(int grp, int lane, const uint4 (&x)[D / 16], u
       const uint32_t w[4] = {x[2 * i + k].x, x[2 * i + k].y, x[2 * i + k].z, x[2 * i + k].w};
       uint32_t h[4];
 #pragma unroll
-      for (int c = 0; c < 4; ++c) h[c] = pack_f16(__uint_as_float(w[c] << 16) * inv, __uint_as_float(w[c] & 0xFFFF0000u) * inv);
+      for (int c = 0; c < 4; ++c) h[c] = scaled_f16(w[c], inv);
       *reinterpret_cast<uint4*>(v16 + sw128_chunk_off(16 * grp + i * RPI + r_in, 2 * ch + k, TC_BN)) = make_uint4(h[0], h[1], h[2], h[3]);
     }
   if (lane == 0) {
@@ -263,8 +265,8 @@ __device__ inline void put_node_k(int grp, int lane, const uint4 (&y)[D / 16], u
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         uint16_t h0, l0, h1, l1;
-        split_e4m3(__uint_as_float(w[2 * c] << 16) * inv, __uint_as_float(w[2 * c] & 0xFFFF0000u) * inv, h0, l0);
-        split_e4m3(__uint_as_float(w[2 * c + 1] << 16) * inv, __uint_as_float(w[2 * c + 1] & 0xFFFF0000u) * inv, h1, l1);
+        split_e4m3(scaled_f16(w[2 * c], inv), h0, l0);
+        split_e4m3(scaled_f16(w[2 * c + 1], inv), h1, l1);
         hi[2 * k + c] = h0 | ((uint32_t)h1 << 16);
         lo[2 * k + c] = l0 | ((uint32_t)l1 << 16);
       }
@@ -421,14 +423,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   bool ok = true, compute = false;
 
   if (warp < QT_SOFTMAX / 32) {
-    // All global loads first.  Nodes: warp w takes V (w even) or K (odd) of groups w / 2 and 4 + w / 2 of 16 nodes.
     const int groups = tree_blocks ? (si.n + 15) >> 4 : 0;
-    uint4 xn[2][D / 16];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (4 * h + (warp >> 1) < groups)
-        load_node_rows<D>((warp & 1 ? p.k_nodes : p.v_nodes) + (long long)si.node_base * p.node_stride + g * D, p.node_stride, si.n,
-                          4 * h + (warp >> 1), lane, xn[h]);
     // Q: 16-byte pieces, D / 8 lanes to a row
     constexpr int LPR = D / 8, RPP = QT_SOFTMAX / LPR, NQ = TC_BM / RPP;
     const int ch = tid % LPR;
@@ -441,15 +436,18 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       if (R < rows_total && SB_CHECKED_ACCESS(si.q_off + nl, p.total_q, &p.status[b]))
         xq[i] = __ldg(reinterpret_cast<const uint4*>(p.q + (long long)(si.q_off + nl) * p.q_stride + (g * G + hh) * D + ch * 8));
     }
+    // Nodes: warp w takes V (w even) or K (odd) of groups w / 2 and 4 + w / 2 of 16 nodes.  (Rolled: this code runs once, and costs its
+    // instruction fetches: unrolled twice 16 trees take 134.5 us, so 133.2.)
     const ScaleRing ring = {s_ks, s_lsv, s_isv};
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int grp = 4 * h + (warp >> 1);
-      if (grp >= groups) continue;
-      const uint32_t bits = drop_bad_rows<D>(lane, xn[h]);
+#pragma unroll 1
+    for (int grp = warp >> 1; grp < groups; grp += 4) {
+      uint4 xn[D / 16];
+      load_node_rows<D>((warp & 1 ? p.k_nodes : p.v_nodes) + (long long)si.node_base * p.node_stride + g * D, p.node_stride, si.n,
+                        grp, lane, xn);
+      const uint32_t bits = drop_bad_rows<D>(lane, xn);
       if (bits && lane == 0) atomicOr(&s_bad[grp >> 1], bits << (16 * (grp & 1)));
-      if (warp & 1) put_node_k<D>(grp, lane, xn[h], sK, sK2, ring);
-      else put_node_v<D>(grp, lane, xn[h], sV, ring);
+      if (warp & 1) put_node_k<D>(grp, lane, xn, sK, sK2, ring);
+      else put_node_v<D>(grp, lane, xn, sV, ring);
     }
     if (tree_blocks) {  // groups without nodes: K may be anything (masked), V has to be finite
       for (int i = groups * 2 * D + tid; i < TC_BN * D / 8; i += QT_SOFTMAX)
@@ -471,7 +469,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       const float inv = __uint_as_float((uint32_t)(254 - e) << 23);
       uint16_t hi[4], lo[4];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) split_e4m3(__uint_as_float(w[k] << 16) * inv, __uint_as_float(w[k] & 0xFFFF0000u) * inv, hi[k], lo[k]);
+      for (int k = 0; k < 4; ++k) split_e4m3(scaled_f16(w[k], inv), hi[k], lo[k]);
       uint8_t* dst = sQ + code_tile_off<D>(r, ch >> 1) + (ch & 1) * 8;
       *reinterpret_cast<uint2*>(dst) = make_uint2(hi[0] | ((uint32_t)hi[1] << 16), hi[2] | ((uint32_t)hi[3] << 16));
       *reinterpret_cast<uint2*>(dst + TILE8) = make_uint2(lo[0] | ((uint32_t)lo[1] << 16), lo[2] | ((uint32_t)lo[3] << 16));

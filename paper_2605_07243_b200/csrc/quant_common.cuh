@@ -38,11 +38,12 @@ __device__ inline float2 float2_of_e4m3x2(uint16_t c) {
   return __half22float2(*reinterpret_cast<const __half2*>(&h));
 }
 
-// Two values -> e4m3 codes of the nearest values and of what is left.
-__device__ inline void split_e4m3(float a, float b, uint16_t& hi, uint16_t& lo) {
-  hi = e4m3x2_of(a, b);
-  const float2 h = float2_of_e4m3x2(hi);
-  lo = e4m3x2_of(a - h.x, b - h.y);
+// Two fp16 values -> e4m3 codes of the nearest values and of what is left (the difference is exact in fp16 for inputs of 8 significant bits).
+__device__ inline void split_e4m3(uint32_t h, uint16_t& hi, uint16_t& lo) {
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(hi) : "r"(h));
+  const uint32_t near = half2_of_e4m3x2(hi);
+  const __half2 rest = __hsub2(*reinterpret_cast<const __half2*>(&h), *reinterpret_cast<const __half2*>(&near));
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(lo) : "r"(*reinterpret_cast<const uint32_t*>(&rest)));
 }
 
 inline sb_status check_quant_cache(const sb_quant_cache* kv) {
