@@ -615,7 +615,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
             if (p.window > 0) word &= low_bits(p.sinks - kq) | ~low_bits(pos - p.window + 1 - kq);
             poison |= ((flags >> (2 * q)) & 1u && (word & 0xFFFFu)) || ((flags >> (2 * q + 1)) & 1u && (word >> 16));
           }
-          mask_scores(s_addr + 32 * q, word);
+          if (__any_sync(0xffffffffu, word != ~0u)) mask_scores(s_addr + 32 * q, word);
         }
       }
       walk(i, group, s_addr);
