@@ -78,10 +78,10 @@ static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree,
   long long keys = tree->max_prefix;  // visible ones, at most
   if (window > 0 && (long long)window + sinks + 64 < keys) keys = (long long)window + sinks + 64;
   const int sms = quant_num_sms();
-  // The 16-row kernel starts and ends in half the time (8 us against 15), but walks the keys once per 16 rows, with the slower matrix
-  // instructions.  us by it and by the tcgen05 kernel, 8 KV heads, groups of 4: 1 to 4 nodes (one tile), 2k keys 11.7 / 20, 64 ragged 8k
-  // prefixes 143 / 242; 16 nodes over 128, 512, 2k keys 10 / 14, 11 / 16, 14 / 20; 32 nodes 11 / 14, 13 / 16.5, 19 / 20.5; 60 nodes
-  // 13 / 14, 17 / 17, 29 / 22; 5 to 8 nodes, 4 ragged 8k prefixes 37 / 36, 16 of them 84 / 74, 64 of them 232 / 209.
+  // The 16-row kernel starts and ends in less time (9 us against 12), but walks the keys once per 16 rows, with the slower matrix
+  // instructions.  us by it and by the tcgen05 kernel, 8 KV heads, groups of 4: 1 to 4 nodes (one tile), 2k keys 11.7 / 18.6, 64 ragged 8k
+  // prefixes 143 / 199; 16 nodes over 128, 512, 2k keys 10 / 12, 11 / 15, 14 / 18; 32 nodes 11 / 12, 13 / 15, 19 / 18.5; 60 nodes
+  // 13 / 13, 17 / 16, 29 / 20; 8 nodes, 4 ragged 8k prefixes 37 / 34, 16 of them 84 / 70, 64 of them 232 / 199.
   const long long tiles = (long long)kv->batch * kv->n_kv_heads * ceil_div(rows, 16);
   pl.tc = rows > 16 && (tiles > 64 || tiles * keys > (1 << 17));
   pl.cluster = 1;
@@ -89,8 +89,8 @@ static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree,
     // A CTA costs its key blocks plus a fixed start and end.  CTAs start longest first on whichever SM is free: equal ones run in waves,
     // ragged ones (three quarters of the longest, taken on average) end about half a chunk unevenly; the estimate lies between the two.
     // Every chunk beyond the first writes and re-reads fp16 partials of all rows, and the merge is one more kernel.  us by 1 / 2 / 3 / 4 /
-    // 6 chunks: one 60-node tree over 2k keys 38 / 30 / 26 / 24 / 22; 8-node trees over ragged 8k prefixes, 4 of them 89 / 54 / 42 / 37 /
-    // 40, 16: 91 / 74 / 82 / 89 / 104, 64: 209 / 244 / 273 / 299 / 355; four full trees, 64 heads, over 32k keys 695 / 724 / 725 / 690 / 772.
+    // 6 chunks: one 60-node tree over 2k keys 34 / 27 / 23 / 21 / 20; 8-node trees over ragged 8k prefixes, 4 of them 79 / 49 / 38 / 34 /
+    // 39, 16: 81 / 70 / 80 / 88 / 107, 64: 199 / 247 / 291 / 327 / 408; four full trees, 64 heads, over 32k keys 651 / 682 / 679 / 643 / 726.
     pl.grid_tiles = ceil_div(rows, 128);
     const int blocks = (int)((keys + 127) / 128) + (window > 0 ? 2 : 0) + 1;
     const double units = (double)kv->batch * kv->n_kv_heads * pl.grid_tiles;

@@ -18,7 +18,8 @@
 // softmax warp always has the next 64 scores waiting while the tensor pipe is busy with the buffer it has just left: with
 // one buffer per stream the warps spent half of their time waiting for PV and S of their own stream.
 // (One tile per CTA, although two tiles could share a key block's loads and conversions: both are off the critical path, which
-// is the exponentials, and the smaller units fill the SMs more evenly: 16 ragged trees 191 -> 150 us.)
+// is the exponentials, and the smaller units fill the SMs more evenly: 191 us against 150 on 16 ragged trees,
+// which take 132 now.)
 //
 // The softmax thread does not compute a maximum after its row's first visible key: the reference is raised when the sum of 32
 // probabilities shows that an exponent is far above it (P' is fp16, which ends at 2^16), a rare event that
