@@ -21,7 +21,7 @@
 // is the exponentials, and the smaller units fill the SMs more evenly: 191 us against 150 on 16 ragged trees,
 // which take 132 now.)
 //
-// The softmax thread does not compute a maximum after its row's first visible key: the reference is raised when the sum of 32
+// The softmax thread does not compute a maximum after its row's first visible key: the reference is raised when the sum of 64
 // probabilities shows that an exponent is far above it (P' is fp16, which ends at 2^16), a rare event that
 // rescales the accumulator.
 //
