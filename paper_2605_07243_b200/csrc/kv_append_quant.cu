@@ -86,9 +86,12 @@ __global__ void __launch_bounds__(kAppendThreads, 4) kv_append_quant_kernel(cons
     if (UT == 32) __syncwarp();
     else asm volatile("barrier.sync %0, %1;" ::"r"(slot + 1), "n"(UT) : "memory");
   };
-  // the same value in every thread of the unit
+  // the same value in every thread of the unit; shared memory that the unit wrote before is complete behind it
   auto any = [slot](bool v) {
-    if (UT == 32) return __any_sync(0xffffffffu, v) != 0;
+    if (UT == 32) {
+      __syncwarp();  // a vote alone orders no memory
+      return __any_sync(0xffffffffu, v) != 0;
+    }
     uint32_t r;
     asm volatile(
         "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.red.or.pred q, %2, %3, p;\n\tselp.u32 %0, 1, 0, q;\n\t}\n"
@@ -124,7 +127,7 @@ __global__ void __launch_bounds__(kAppendThreads, 4) kv_append_quant_kernel(cons
       s_path[slot][i] = self;
       bad |= self < 0 || self >= avail || (i > 0 && path[i - 1] >= self);
     }
-    if (any(bad)) err = SB_ERR_INVALID_TREE;                  // (also a barrier: s_path is complete)
+    if (any(bad)) err = SB_ERR_INVALID_TREE;                  // (s_path is complete from here on)
   }
   const int lo = (int)(t0 > start ? t0 : start) - (int)t0;    // new rows of the block: [lo, hi)
   const int hi = mine ? (int)min((long long)start + n - t0, (long long)sb) : 0;
