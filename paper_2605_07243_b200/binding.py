@@ -654,9 +654,9 @@ class QuantTree:
         object.__setattr__(self, "total_nodes", self.parent.numel())
 
 
-def _rows_of(t, heads, dim, device, what):
+def _rows_of(t, heads, dim, device, what, dims=3):
     """(address, elements between rows) of bf16 rows [..., heads, dim] whose rows are contiguous inside: a whole tensor or
-    a slice of a fused projection."""
+    a slice of a fused projection, of `dims` dimensions (the caller sees to those before the rows)."""
     if t.dtype is not torch.bfloat16:
         raise TypeError(f"{what}: expected torch.bfloat16, got {t.dtype}")
     if t.get_device() != device:
@@ -666,10 +666,16 @@ def _rows_of(t, heads, dim, device, what):
         raise ValueError(f"{what}: expected rows of [{heads}, {dim}], got {tuple(shape)}")
     if t.is_contiguous():
         return t.data_ptr(), heads * dim
+    if len(shape) != dims:
+        raise ValueError(f"{what}: expected strided rows in {dims} dimensions, got {tuple(shape)}")
     stride = t.stride()
     if stride[-1] != 1 or (heads > 1 and stride[-2] != dim):
         raise ValueError(f"{what}: expected rows that are contiguous inside, got strides {stride}")
-    return t.data_ptr(), (stride[-3] if shape[-3] > 1 else heads * dim)
+    if shape[-3] <= 1:
+        return t.data_ptr(), heads * dim
+    if stride[-3] < heads * dim:  # an expanded tensor: 0 means "one row behind the other" to the library, past the tensor's end
+        raise ValueError(f"{what}: expected rows that do not overlap, got strides {stride}")
+    return t.data_ptr(), stride[-3]
 
 
 def sb_tree_attention_quant_workspace_bytes(kv: QuantCache, tree: QuantTree, total_q: int, *, num_splits: int = 0,
@@ -736,8 +742,8 @@ def sb_kv_append_quant(kv: QuantCache, k_rows, v_rows, row_offsets, length, *, m
         layer_stride = 0
     else:
         raise ValueError("rows must be [layers, rows, n_kv_heads, head_dim]")
-    k_ptr, stride = _rows_of(k_rows, kv.n_kv_heads, kv.head_dim, dev, "k_rows")
-    v_ptr, _ = _rows_of(v_rows, kv.n_kv_heads, kv.head_dim, dev, "v_rows")
+    k_ptr, stride = _rows_of(k_rows, kv.n_kv_heads, kv.head_dim, dev, "k_rows", k_rows.dim())
+    v_ptr, _ = _rows_of(v_rows, kv.n_kv_heads, kv.head_dim, dev, "v_rows", k_rows.dim())
     new_len = torch.empty(B, dtype=torch.int32, device=dev) if new_len is None else new_len
     status = torch.empty(B, dtype=torch.int32, device=dev) if status is None else status
     rc = load().sb_kv_append_quant(

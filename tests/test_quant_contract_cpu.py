@@ -1,0 +1,27 @@
+"""Host side of the calls over 8-bit caches and pages: calls whose tensors the library cannot be told of.  No GPU."""
+import pytest
+import torch
+
+from paper_2605_07243_b200 import binding as sb
+
+
+def test_rows_that_overlap_are_refused():
+    """An expanded tensor has a stride of 0 between its rows, which to the library is the ordinary one."""
+    one = torch.zeros(1, 2, 64, dtype=torch.bfloat16)
+    for rows in (one.expand(5, 2, 64), torch.zeros(1024, dtype=torch.bfloat16).as_strided((5, 2, 64), (64, 64, 1)),
+                 torch.zeros(4, 1, 2, 64, dtype=torch.bfloat16).expand(4, 3, 2, 64)):
+        with pytest.raises(ValueError, match="overlap"):
+            sb._rows_of(rows, 2, 64, -1, "rows", rows.dim())
+    assert sb._rows_of(one.expand(1, 2, 64), 2, 64, -1, "rows") == (one.data_ptr(), 128)
+    fused = torch.zeros(5, 7, 64, dtype=torch.bfloat16)
+    assert sb._rows_of(fused[:, 3:5], 2, 64, -1, "rows") == (fused.data_ptr() + 2 * 3 * 64, 7 * 64)
+    # layers may repeat: their stride has its own argument
+    assert sb._rows_of(fused[None, :, 3:5].expand(4, 5, 2, 64), 2, 64, -1, "rows", 4)[1] == 7 * 64
+
+
+def test_strided_rows_of_other_dimensions_are_refused():
+    """[rows, 1, heads, dim] as a slice: the stride that counts is not the one before the heads."""
+    fused = torch.zeros(5, 1, 7, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="dimensions"):
+        sb._rows_of(fused[:, :, 3:5], 2, 64, -1, "rows")
+    assert sb._rows_of(fused, 7, 64, -1, "rows") == (fused.data_ptr(), 7 * 64)
