@@ -594,7 +594,8 @@ sb_status sb_pages_fork(const sb_page_pool* pool, int32_t n, const int32_t* src,
                         void* stream);
 
 /* sb_pages_reserve -- makes positions [keep_len[i], new_len[i]) of slots[i] writable: pages are added up to new_len,
- * and a page that holds any of these positions and is shared becomes the slot's own.  When every holder of a
+ * and a page that holds any of these positions and is shared becomes the slot's own.  An empty range (keep_len = new_len,
+ * wherever it lies) holds none: such an entry asks for nothing and writes nothing.  When every holder of a
  * shared page is served by this call the first of them in the list keeps it.  If the
  * replaced page also holds positions below keep_len (at most one page per slot does) the pair (old page, new
  * page) is appended to the copy list, for sb_pages_copy to copy the contents.

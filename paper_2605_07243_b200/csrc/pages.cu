@@ -147,6 +147,13 @@ __global__ void __launch_bounds__(PG_THREADS) pages_fork_kernel(const sb_page_po
   }
 }
 
+// The logical pages [first, last) that hold positions [keep, upto) of a slot: none for an empty range, wherever it lies.
+struct PageRange {
+  int first, last;
+  __device__ PageRange(int keep, int upto, int page_size)
+      : first(keep / page_size), last(upto > keep ? pages_for(upto, page_size) : first) {}
+};
+
 struct ReserveWs {
   int *claim, *count, *first_of, *free_ids, *want, *copies;
   __device__ ReserveWs(int* ws, const sb_page_pool& pool, int n) {
@@ -187,10 +194,11 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const sb_page
       if (keep < 0 || upto < keep || held < 0 || held > pool.max_pages) err = SB_ERR_BOUNDS;
       else if (pages_for(upto, ps) > pool.max_pages || pages_for(keep, ps) > held) err = SB_ERR_BOUNDS;
       else {
-        const int first = keep / ps, last = min(held, pages_for(upto, ps));
-        if (!pages_sound(pool, s, first, last)) err = SB_ERR_BOUNDS;
+        const PageRange r(keep, upto, ps);
+        const int last = min(held, r.last);
+        if (!pages_sound(pool, s, r.first, last)) err = SB_ERR_BOUNDS;
         else
-          for (int p = first + lane; p < last; p += 32) {
+          for (int p = r.first + lane; p < last; p += 32) {
             const int page = pool.page_table[(long long)s * pool.max_pages + p];
             atomicAdd(&ws.count[page], 1);
             atomicMin(&ws.first_of[page], i);
@@ -209,15 +217,16 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const sb_page
     int wants = 0, copies = 0;
     if (status[i] == 0) {
       const int s = slots[i], keep = keep_len[i], held = pool.held[s];
-      const int first = keep / ps, last = pages_for(new_len[i], ps);
+      const PageRange r(keep, new_len[i], ps);
+      const int last = min(held, r.last);
       const int* row = pool.page_table + (long long)s * pool.max_pages;
-      for (int p0 = first; p0 < min(held, last); p0 += 32) {
+      for (int p0 = r.first; p0 < last; p0 += 32) {
         const int p = p0 + lane;
-        const bool rep = p < min(held, last) && replaced(row[p], i);
+        const bool rep = p < last && replaced(row[p], i);
         wants += __popc(__ballot_sync(0xffffffffu, rep));
         copies += __popc(__ballot_sync(0xffffffffu, rep && (long long)p * ps < keep));
       }
-      wants += max(0, last - max(held, first));
+      wants += max(0, r.last - max(held, r.first));
     }
     if (lane == 0) {
       ws.want[i] = wants;
@@ -275,10 +284,11 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const sb_page
     const bool on = i < n && status[i] == 0 && ws.want[i] >= 0;
     if (on) {
       const int s = slots[i], keep = keep_len[i], held = pool.held[s];
-      const int first = keep / ps, last = pages_for(new_len[i], ps);
+      const PageRange r(keep, new_len[i], ps);
+      const int last = r.last;
       int* row = pool.page_table + (long long)s * pool.max_pages;
       int rank = ws.want[i];
-      for (int p0 = first; p0 < last; p0 += 32) {
+      for (int p0 = r.first; p0 < last; p0 += 32) {
         const int p = p0 + lane;
         // ... and each replacement is noted in the table as -2 - fresh until every warp has decided
         const bool have = p < min(held, last);
@@ -303,9 +313,11 @@ __global__ void __launch_bounds__(PG_THREADS) pages_reserve_kernel(const sb_page
   __syncthreads();
   for (int i = warp; i < n; i += PG_WARPS) {
     if (status[i] || ws.want[i] < 0) continue;
-    const int s = slots[i], first = keep_len[i] / ps, last = pages_for(new_len[i], ps);
+    const int s = slots[i];
+    const PageRange r(keep_len[i], new_len[i], ps);
+    const int last = r.last;
     int* row = pool.page_table + (long long)s * pool.max_pages;
-    for (int p = first + lane; p < last; p += 32) {
+    for (int p = r.first + lane; p < last; p += 32) {
       const int noted = row[p];
       if (noted <= -2) {
         const int fresh = -2 - noted, old = ws.first_of[fresh];

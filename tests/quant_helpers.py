@@ -201,6 +201,10 @@ class Pool:
     def pages(self, n):
         return -(-n // self.ps)
 
+    def written(self, keep, new):
+        """Logical pages that hold a position of [keep, new)."""
+        return range(keep // self.ps, self.pages(new)) if new > keep else range(0)
+
     def _named(self, slots):
         seen, first = set(), []
         for s in slots:
@@ -246,10 +250,11 @@ class Pool:
         writers = {}
         for i, (s, k, n, e) in enumerate(zip(slots, keep, new, st)):
             if e == OK:
-                for p in range(k // self.ps, min(len(self.rows[s]), self.pages(n))):
-                    writers.setdefault(self.rows[s][p], []).append(i)
+                for p in self.written(k, n):
+                    if p < len(self.rows[s]):
+                        writers.setdefault(self.rows[s][p], []).append(i)
         for i, (s, k, n, e) in enumerate(zip(slots, keep, new, st)):
-            for p in range(k // self.ps, self.pages(n)) if e == OK else []:
+            for p in self.written(k, n) if e == OK else []:
                 if p >= len(self.rows[s]):
                     wishes.append((i, s, p, None))
                 else:

@@ -32,3 +32,30 @@ def test_append_paths_as_long_as_they_come(block, depth):
         new_len, status = sb.sb_kv_append_quant(kv, kg, vg, i32(offs), i32(P), **args)
         assert status.cpu().tolist() == [0] * len(P) and new_len.cpu().tolist() == want
         same_cache(kv, cache)
+
+
+# ---- pages ----------------------------------------------------------------------------------------------------------------
+
+def test_pages_reserve_of_an_empty_range_asks_for_nothing():
+    """[20, 20) holds no position: the slot takes no page, is no writer of the page that it shares, and is served by a full pool."""
+    pool = sb.PagePool.empty(4, 4, 4, 16)
+    copies = sb.PageCopies.empty(2)
+    state = lambda: [t.cpu().tolist() for t in (pool.page_table, pool.held, pool.refs)]   # noqa: E731
+    assert sb.sb_pages_reserve(pool, i32([0]), i32([0]), i32([20]), copies).tolist() == [0]
+    assert sb.sb_pages_fork(pool, i32([0]), i32([1]), i32([20])).tolist() == [0]
+    before = state()
+    assert before[0][1][:2] == [0, 1] and before[2] == [2, 2, 0, 0]
+    for at in (20, 16, 1, 0):
+        assert sb.sb_pages_reserve(pool, i32([1]), i32([at]), i32([at]), copies).tolist() == [0]
+        assert state() == before and copies.count.item() == 0 and copies.src.tolist() == [-1, -1]
+    assert sb.sb_pages_reserve(pool, i32([2]), i32([0]), i32([32]), copies).tolist() == [0]      # the pool is full
+    before = state()
+    assert sb.sb_pages_reserve(pool, i32([1]), i32([20]), i32([20]), copies).tolist() == [0]
+    assert sb.sb_pages_reserve(pool, i32([1, 0]), i32([20, 20]), i32([20, 21]), copies).tolist() == [0, 7]
+    assert state() == before and copies.count.item() == 0
+    assert sb.sb_pages_release(pool, i32([2]), i32([0])).tolist() == [0]
+    # slot 0 writes a page that slot 1 goes on holding: it gets one of its own
+    assert sb.sb_pages_reserve(pool, i32([1, 0]), i32([20, 20]), i32([20, 21]), copies).tolist() == [0, 0]
+    assert copies.count.item() == 1 and copies.src.tolist() == [1, -1] and copies.dst.tolist() == [2, -1]
+    table, held, refs = state()
+    assert table[0] == [0, 2, -1, -1] and table[1] == [0, 1, -1, -1] and held == [2, 2, 0, 0] and refs == [2, 1, 1, 0]
