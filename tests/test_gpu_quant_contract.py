@@ -10,6 +10,8 @@ from test_gpu_quant import append_case, check, i32, make, same_cache, tree_of
 
 pytestmark = pytest.mark.gpu
 
+KERNELS = [(2, 2, 2, 20), (6, 8, 2, 50)]     # sequences, KV heads, heads of each, nodes: 16-row kernel, tcgen05 kernel
+
 
 # ---- append ---------------------------------------------------------------------------------------------------------------
 
@@ -59,3 +61,21 @@ def test_pages_reserve_of_an_empty_range_asks_for_nothing():
     assert copies.count.item() == 1 and copies.src.tolist() == [1, -1] and copies.dst.tolist() == [2, -1]
     table, held, refs = state()
     assert table[0] == [0, 2, -1, -1] and table[1] == [0, 1, -1, -1] and held == [2, 2, 0, 0] and refs == [2, 1, 1, 0]
+
+
+# ---- attention ------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("batch,H,G,n", KERNELS)
+@pytest.mark.parametrize("num_splits", [0, 1])
+@pytest.mark.parametrize("log_v", [-12, -30, 20])
+@pytest.mark.parametrize("gap", [0.0, 6.0, 9.0])
+def test_attention_nodes_far_above_the_prefix_keep_its_share(batch, H, G, n, num_splits, log_v, gap):
+    """Every node's score of itself lies `gap` above the others, and values are small or large: the prefix keeps its weight."""
+    P = [[700, 0, 77, 513][b % 4] for b in range(batch)]
+    cache, parents, q, k, v = make(74, P, [n] * batch, H=H, G=G, D=64, v_mag=2.0 ** log_v)
+    v = (v.float() * 2.0 ** log_v).bfloat16()
+    cache.scales[0][:] *= 2.0 ** -6                                     # prefix scores near zero
+    cache.scales[1][:] = 2.0 ** (log_v - 6)
+    q = torch.ones_like(q)
+    k = torch.full_like(k, gap / 8)
+    check(cache, P, parents, q, k, v, num_splits=num_splits)
