@@ -20,8 +20,8 @@
 // scaled.  The reference of a row is its largest exponent of the first keys that it sees and is raised only when a sum
 // shows that an exponent lies far above it, so that the common step needs no maximum and no shuffle.
 //
-// The tree's nodes come first in the key list, in groups of 16 bf16 rows that go straight from global memory into bf16 products
-// (a V row times a power of two, which enters the exponent as a block's scale does): the first codes are on their way meanwhile.
+// The tree's nodes come first in the key list, in groups of 16 bf16 rows that go straight from global memory into bf16 products:
+// the first codes are on their way meanwhile.
 //
 // Chunks of one tile are merged inside a cluster through distributed shared memory (up to 8), further clusters by
 // quant_merge_kernel.
@@ -249,10 +249,8 @@ __global__ void __launch_bounds__(QR_THREADS, 3) quant_rows_kernel(const QuantAt
   bool seen_any[2] = {false, false};               // the row has met a visible key, and `ref` is its reference
 
   // Exponents a[t][e] of two or four 8-key tiles (base 2, V scale folded in, relative to the reference, masked to -inf) -> probabilities.
-  // inv_v: 1 / V scale, of the two 16-key halves of four tiles of codes, or of a node's columns [tile][column] of two.
-  auto softmax_step = [&](auto& a, const auto& inv_v) {
+  auto softmax_step = [&](auto& a, const float (&inv_v)[2]) {  // inv_v: of the two halves of the tiles
     constexpr int T = (int)(sizeof(a) / sizeof(a[0]));
-    constexpr bool PER_KEY = sizeof(inv_v) / sizeof(inv_v[0]) == 4;
     bool raise = !(seen_any[0] && seen_any[1]);
     float pr[T][4], sum[2][2];
     while (true) {
@@ -302,16 +300,10 @@ __global__ void __launch_bounds__(QR_THREADS, 3) quant_rows_kernel(const QuantAt
 #pragma unroll
       for (int e = 0; e < 4; ++e) a[t][e] = pr[t][e];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      if constexpr (PER_KEY) {
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) l[h] = fmaf(pr[x >> 1][2 * h + (x & 1)], inv_v[x], l[h]);
-      } else {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-          if (sum[h][u] != 0.f) l[h] = fmaf(sum[h][u], inv_v[u], l[h]);  // a NaN scale must not meet an empty half
-      }
-    }
+      for (int u = 0; u < 2; ++u)
+        if (sum[h][u] != 0.f) l[h] = fmaf(sum[h][u], inv_v[u], l[h]);  // a NaN scale must not meet an empty half
   };
 
   // ---- nodes -------------------------------------------------------------------------------------------------------------
@@ -357,31 +349,6 @@ __global__ void __launch_bounds__(QR_THREADS, 3) quant_rows_kernel(const QuantAt
       if (nf) bad |= 1u << (8 * (x >> 1) + key_of_col<D>(2 * fc + (x & 1)));
     }
     bad = __reduce_or_sync(0xffffffffu, bad);
-    // A V row's power of two 2^lsv takes its largest element to 2^8 .. 2^9, where a block's scale takes its codes.  Without it a reference
-    // that comes from nodes would not be the one of the products P V, and the prefix's fp16 probabilities would sink below it
-    // by the scale of their block (values of 2^-7: scale 2^-15).  Between 2^-60 and 2^40, as the scales are: exponents of two keys that count
-    // alike then lie less than fp32's range apart.
-    float lsv[4], inv_v[4];
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      if ((bad >> (8 * (x >> 1) + key_of_col<D>(2 * fc + (x & 1)))) & 1u)  // counts through its NaN probability; its elements must not meet the zeros of other rows
-#pragma unroll
-        for (int k = 0; k < NT / 2; ++k) vw[x][k] = 0;
-      uint32_t amax = 0;
-#pragma unroll
-      for (int k = 0; k < NT / 2; ++k) amax = __vmaxu2(amax, vw[x][k] & 0x7FFF7FFFu);
-#pragma unroll
-      for (int d = 4; d < 32; d <<= 1) amax = __vmaxu2(amax, __shfl_xor_sync(0xffffffffu, amax, d));
-      const int e = min(max((int)(max(amax & 0xFFFFu, amax >> 16) >> 7) - 8, 127 - 60), 127 + 40);  // biased; see v_scale_used
-      lsv[x] = (float)(e - 127);
-      inv_v[x] = __uint_as_float((uint32_t)(254 - e) << 23);
-      const __nv_bfloat162 f = __float2bfloat162_rn(inv_v[x]);
-#pragma unroll
-      for (int k = 0; k < NT / 2; ++k) {
-        const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&vw[x][k]), f);  // exact
-        vw[x][k] = *reinterpret_cast<const uint32_t*>(&y);
-      }
-    }
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -392,10 +359,17 @@ __global__ void __launch_bounds__(QR_THREADS, 3) quant_rows_kernel(const QuantAt
           const int kp = si.P + s_depth[nd];
           seen = kp < p.sinks || pos[h] - kp < p.window;
         }
-        a[t][e] = seen ? (((bad >> kk) & 1u) ? __uint_as_float(0x7FC00000u) : fmaf(a[t][e], p.scale_log2, lsv[2 * t + (e & 1)] - ref[h])) : -INFINITY;
+        a[t][e] = seen ? (((bad >> kk) & 1u) ? __uint_as_float(0x7FC00000u) : fmaf(a[t][e], p.scale_log2, -ref[h])) : -INFINITY;
       }
-    softmax_step(a, inv_v);
+    const float one[2] = {1.f, 1.f};
+    softmax_step(a, one);
     const uint32_t pa[4] = {pack_bf16(a[0][0], a[0][1]), pack_bf16(a[0][2], a[0][3]), pack_bf16(a[1][0], a[1][1]), pack_bf16(a[1][2], a[1][3])};
+    // a bad row counts through its NaN probability; its elements must not meet the zeros of other rows
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      if ((bad >> (8 * (x >> 1) + key_of_col<D>(2 * fc + (x & 1)))) & 1u)
+#pragma unroll
+        for (int k = 0; k < NT / 2; ++k) vw[x][k] = 0;
 #pragma unroll
     for (int k = 0; k < NT / 2; ++k) {
       mma_bf16(o[2 * k], pa, __byte_perm(vw[0][k], vw[1][k], 0x5410), __byte_perm(vw[2][k], vw[3][k], 0x5410));
@@ -423,6 +397,23 @@ __global__ void __launch_bounds__(QR_THREADS, 3) quant_rows_kernel(const QuantAt
 #pragma unroll
       for (int x = 0; x < 2; ++x)
         qa[k][2 * x + h] = pack_half(__uint_as_float(qa[k][2 * x + h] << 16) * inv, __uint_as_float(qa[k][2 * x + h] & 0xFFFF0000u) * inv);
+  }
+  // A reference that comes from nodes knows nothing of the V scale that the codes' exponents contain: with small values (of 2^-7: scale
+  // 2^-15) the fp16 probabilities of the prefix would lie that far below it.  It goes down by the scale of the first codes.
+  if (nodes_mine > 0 && codes_mine > 0) {
+    asm volatile("cp.async.wait_group %0;\n" ::"n"(QR_STAGES - 1) : "memory");
+    __syncwarp();
+    const float down = fminf(__log2f(v_scale_used(fminf(s_scale[warp][0][2], s_scale[warp][0][3]))), 0.f);
+    const float f = fast_exp2(-down);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      ref[h] += down;
+      l[h] *= f;
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[t][e] *= f;
   }
   bool ok = true;
   for (int i = 0; i < codes_mine; ++i) {
