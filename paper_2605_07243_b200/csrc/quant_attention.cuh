@@ -99,6 +99,16 @@ __device__ inline BlockList visible_blocks(int P, int window, int sinks, int siz
   return l;
 }
 
+// The prefix positions that no node of the sequence sees: [lo, hi), between the sinks and the window of a node at depth 0; empty
+// without a window.  What a block of keys holds there may be anything, codes that are NaN included: V codes must not meet
+// the zero probabilities.
+struct UnseenKeys {
+  int lo, hi;
+  __device__ UnseenKeys(int P, int window, int sinks) : lo(sinks), hi(window > 0 ? P - window + 1 : 0) {}
+  __device__ bool meets(int first, int last) const { return max(first, lo) < min(last, hi); }  // of the keys [first, last)
+  __device__ bool has(int j) const { return j >= lo && j < hi; }
+};
+
 // Sequence with rank z by length, longest first (see sequence_of_rank in attention_common.cuh).  batch <= SB_MAX_NODES; s_len: 16-byte
 // aligned scratch of SB_MAX_NODES ints, s_pick: one int.
 __device__ inline int quant_sequence_of_rank(const QuantAttnParams& p, int z, int* s_len, int* s_pick) {

@@ -104,6 +104,18 @@ __device__ inline void load_row_share(uint32_t (&w)[D / 8], const bf16* row, int
     }
 }
 
+// Zeros over the rows of a V tile (keys k0 .. k0 + 31) that no node sees, behind the prefix or before every window: what lies there (stale
+// bytes, codes that are NaN) must not meet the zero probabilities.  One warp.
+template <int D>
+__device__ __forceinline__ void clear_unseen(uint32_t tile, int k0, int P, const UnseenKeys unseen, int lane) {
+  for (int c = lane; c < QR_GROUP * (D / 16); c += 32) {
+    const int j = k0 + c / (D / 16);
+    if (j >= P || unseen.has(j)) asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(tile + c * 16), "r"(0) : "memory");
+  }
+  fence_async_smem();  // a later load into the stage comes after these writes
+  __syncwarp();
+}
+
 template <int D>
 __global__ void __launch_bounds__(QR_THREADS, 3) quant_rows_kernel(const QuantAttnParams p, const __grid_constant__ CUtensorMap kmap,
                                                                    const __grid_constant__ CUtensorMap vmap, const int box_rows,
@@ -422,12 +434,9 @@ __global__ void __launch_bounds__(QR_THREADS, 3) quant_rows_kernel(const QuantAt
     if (ok) ok = mbar_wait(&s_full[warp][i % QR_STAGES], (i / QR_STAGES) & 1, &s_abort);
     asm volatile("cp.async.wait_group %0;\n" ::"n"(QR_STAGES - 1) : "memory");
     __syncwarp();
-    if (k0 + QR_GROUP > si.P) {  // the prefix ends here: stale V bytes behind it must not meet the zero probabilities
-      const int left = si.P - k0;
-      for (int c = lane; c < (QR_GROUP - left) * (D / 16); c += 32)
-        *reinterpret_cast<uint4*>(smem + (stage - smem_u32(smem)) + QR_GROUP * D + (left * D + c * 16)) = make_uint4(0, 0, 0, 0);
-      __syncwarp();
-    }
+    const bool all_seen = k0 + QR_GROUP <= si.P &&
+                          (p.window == 0 || k0 + QR_GROUP <= p.sinks || si.P + si.n - 1 - k0 < p.window);
+    if (!all_seen) clear_unseen<D>(stage + QR_GROUP * D, k0, si.P, UnseenKeys(si.P, p.window, p.sinks), lane);
     float a[4][4];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
@@ -461,8 +470,6 @@ __global__ void __launch_bounds__(QR_THREADS, 3) quant_rows_kernel(const QuantAt
       lsv[u] = __log2f(sv);
       inv_v[u] = __fdividef(1.f, sv);
     }
-    const bool all_seen = k0 + QR_GROUP <= si.P &&
-                          (p.window == 0 || k0 + QR_GROUP <= p.sinks || si.P + si.n - 1 - k0 < p.window);
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll

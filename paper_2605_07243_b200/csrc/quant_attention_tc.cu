@@ -755,6 +755,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     const int cw = warp - QT_CVT_WARP;
     constexpr int CPR = D / 16, RPI = 32 / CPR, NI = 32 / RPI;
     const int ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
+    const UnseenKeys unseen(si.P, p.window, p.sinks);
     for (int j = tree_blocks; j < nb; ++j) {
       const int st = (j - tree_blocks) % 3, use = (j - tree_blocks) / 3;
       uint8_t* stage = sV + (j & 1) * TILE;
@@ -763,7 +764,8 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       const uint8_t* raw = sVr + st * TILE8;
-      const int left = si.P - prefix_key(j);
+      const int k0 = prefix_key(j), left = si.P - k0;
+      const bool gap = unseen.meets(k0, k0 + TC_BN);
       const uint32_t tiny = (s_flag[j & 7] >> 8) & 255u;
 #pragma unroll 1
       for (int q = 0; q < 2; ++q) {
@@ -771,11 +773,11 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
         uint4 x[NI];
 #pragma unroll
         for (int i = 0; i < NI; ++i) x[i] = *reinterpret_cast<const uint4*>(raw + code_tile_off<D>(r0 + i * RPI + r_in, ch));
-        if (left < r0 + 32 || tiny) {  // rows past the prefix (stale bytes), and blocks that read as zeros
+        if (left < r0 + 32 || tiny || gap) {  // rows past the prefix (stale bytes) or before every window, and blocks that read as zeros
 #pragma unroll
           for (int i = 0; i < NI; ++i) {
             const int r = r0 + i * RPI + r_in;
-            if (r >= left || ((tiny >> (r >> 4)) & 1u)) x[i] = make_uint4(0, 0, 0, 0);
+            if (r >= left || ((tiny >> (r >> 4)) & 1u) || unseen.has(k0 + r)) x[i] = make_uint4(0, 0, 0, 0);
           }
         }
 #pragma unroll

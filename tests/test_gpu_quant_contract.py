@@ -79,3 +79,20 @@ def test_attention_nodes_far_above_the_prefix_keep_its_share(batch, H, G, n, num
     q = torch.ones_like(q)
     k = torch.full_like(k, gap / 8)
     check(cache, P, parents, q, k, v, num_splits=num_splits)
+
+
+@pytest.mark.parametrize("batch,H,G,n", KERNELS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(70, 0), (70, 5), (33, 130), (1, 1)])
+def test_attention_nan_codes_before_the_window_do_not_matter(batch, H, G, n, D, window, sinks):
+    """Rows between the sinks and the window of the root hold e4m3's NaN: no node sees them."""
+    P = [[300, 200, 77, 513][b % 4] for b in range(batch)]
+    cache, parents, q, k, v = make(73, P, [n] * batch, H=H, G=G, D=D, block=32)
+    want, wlse = check(cache, P, parents, q, k, v, window=window, sinks=sinks)
+    for b in range(batch):
+        rows = [cache.row(b, j) for j in range(sinks, max(sinks, P[b] - window + 1))]
+        for c in cache.codes:
+            c[0, rows] = 0x7F + 0x80 * (np.arange(H * D).reshape(H, D) & 1)
+    out, lse, status = sb.sb_tree_attention_quant(cache.gpu(sb), tree_of(P, parents, q.shape[1]), q.cuda(), k.cuda(), v.cuda(), window=window, sinks=sinks)
+    assert status.tolist() == [0] * batch
+    assert torch.equal(out, want) and torch.equal(lse, wlse)
