@@ -523,7 +523,11 @@ typedef struct sb_quant_tree {
  *   A node row of K or V that holds a NaN or an infinity makes the outputs of the nodes that see it NaN and
  *   changes no other node's.  Scores, softmax and outputs are accumulated in fp32.  The codes enter the products as
  *   they are; Q, scaled by a power of two per row, as fp16 or as two e4m3 terms; node rows as bf16, or scaled by a
- *   power of two per 16 nodes (K as two e4m3 terms, V as fp16); the probabilities as fp16 (of node rows: fp16 or bf16).
+ *   power of two per row (K as two e4m3 terms, V as fp16); the probabilities as fp16 (of node rows: fp16 or bf16).  What a
+ *   node does not see changes nothing of its result but the rounding.  The two terms lose at most 2^-17 of the largest
+ *   element of their row; a probability times its V scale (of a node: the power of two) loses at most 2^-11 of itself (bf16:
+ *   2^-9), or 2^-25 of the row's largest probability times the largest scale it sees if that is more.  Finite V rows of nodes
+ *   are below 2^56.
  *   workspace: sb_tree_attention_quant_workspace_bytes(...) bytes, 256-byte aligned, no initialisation; calls
  *   that may overlap on the GPU need distinct workspaces.
  */

@@ -26,7 +26,8 @@
 // rescales the accumulator.
 //
 // The tree's nodes are one block of their own, the first of the list: the softmax warps bring it into the first stages before anything
-// else, scaled by a power of two per 16 rows as if they were codes (K as two e4m3 terms, V as fp16).  Then come the prefix
+// else, scaled by a power of two per row as if they were codes (K as two e4m3 terms, V as fp16).  Its step has a function of its
+// own in front of the loop, since its columns have a scale each; in the loop the same test cost 2 % of the long trees.  Then come the prefix
 // blocks of 128 keys that the window leaves.
 #include "quant_attention.cuh"
 
@@ -141,6 +142,12 @@ __device__ inline void tmem_wait_ld(uint32_t (&r)[32]) {
                : "memory");
 }
 
+__device__ inline float4 lds_float4(uint32_t a) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
+  return v;
+}
+
 // Rescales a row's accumulator in tensor memory.  Rare, and out of line: its registers and code stay out of the main loop.
 template <int D>
 static __device__ __noinline__ void rescale_row(uint32_t o_addr, float factor) {
@@ -166,11 +173,6 @@ template <int D>
 __device__ inline uint32_t code_tile_off(int r, int ch) {
   return (uint32_t)(r * D + ((ch ^ (D == 128 ? (r & 7) : ((r >> 1) & 3))) << 4));
 }
-struct ScaleRing {
-  // Eight slots: the loader writes block j's when S of block j - 3 is done, i.e. the softmax with block j - 5.
-  float *ks, *lsv, *isv;   // [8 slots][8 groups of 16 keys]: K scale, log2 of the V scale, 1 / V scale
-};
-
 // Lane -> (row, 16-element chunk) when a warp moves rows of D elements, 32 / (D / 16) rows at a time.  D = 128: eight neighbouring
 // lanes hold four chunks of one row and the other four of the next: 16-byte codes that lie in different banks, and so do the fp16 halves
 // that they become (a row's two fp16 column halves share their banks, two neighbouring rows do not).
@@ -216,49 +218,66 @@ __device__ inline uint32_t drop_bad_rows(int lane, uint4 (&x)[D / 16]) {
       if ((bits >> (i * RPI + r_in)) & 1u) x[2 * i] = x[2 * i + 1] = make_uint4(0, 0, 0, 0);
   return bits;
 }
-// Biased exponent e of the power of two 2^(e - 127) that takes 16 rows to magnitudes below 2^(up + 1).
-template <int N>
-__device__ inline int node_exponent(const uint4 (&x)[N], int up, int least) {
-  uint32_t amax = 0;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-    for (int k = 0; k < 4; ++k) amax = max(amax, max(w[k] & 0x7FFFu, (w[k] >> 16) & 0x7FFFu));
-  }
-  amax = __reduce_max_sync(0xffffffffu, amax);
-  return min(amax < 0x80u ? 127 : max((int)(amax >> 7) - up, least), 253);
-}
-// 16 rows of the tree (group grp), one warp: V as fp16, or K as two e4m3 terms, and their scale (slot 0 of the ring).
+// For each of this lane's rows the biased exponent e of the power of two 2^(e - 127) that takes the row's magnitudes below 2^(up + 1).  A row has
+// an exponent of its own: of a tree's nodes only ancestors see each other, and a common one would let a large row cost the bits of
+// rows beside it (one for 16 rows: a sibling 2^12 times larger moved scores by 0.07, one 2^16 times larger by 1.2).
 template <int D>
-__device__ inline void put_node_v(int grp, int lane, const uint4 (&x)[D / 16], uint8_t* v16, ScaleRing ring) {
+__device__ inline void node_exponents(const uint4 (&x)[D / 16], int up, int least, int (&e)[D / 32]) {
+  constexpr int NI = D / 32;
+#pragma unroll
+  for (int i = 0; i < NI; i += 2) {
+    uint32_t m[2];
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const uint4 a = x[2 * (i + k)], b = x[2 * (i + k) + 1];
+      const uint32_t w = __vmaxu2(__vmaxu2(__vmaxu2(a.x & 0x7FFF7FFFu, a.y & 0x7FFF7FFFu), __vmaxu2(a.z & 0x7FFF7FFFu, a.w & 0x7FFF7FFFu)),
+                                  __vmaxu2(__vmaxu2(b.x & 0x7FFF7FFFu, b.y & 0x7FFF7FFFu), __vmaxu2(b.z & 0x7FFF7FFFu, b.w & 0x7FFF7FFFu)));
+      m[k] = max(w & 0xFFFFu, w >> 16);
+    }
+    uint32_t both = m[0] | (m[1] << 16);
+    both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 1));
+    both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 2));
+    if (D == 128) both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 8));  // (see lane_row)
+    e[i] = max((int)((both & 0xFFFFu) >> 7) - up, least);
+    e[i + 1] = max((int)(both >> 23) - up, least);
+  }
+}
+// What the step over the tree needs of a node's rows: 2^e of K and the exponent of V's power of two.
+struct NodeScales {
+  float *k, *log_v;
+};
+// 16 rows of the tree (group grp), one warp: V as fp16, or K as two e4m3 terms, and their scales.
+template <int D>
+__device__ inline void put_node_v(int grp, int lane, const uint4 (&x)[D / 16], uint8_t* v16, NodeScales scales) {
   constexpr int RPI = 512 / D, NI = 16 / RPI;
   const int ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
-  const int ev = node_exponent(x, 8, 127 - 60);  // (see v_scale_used)
-  const float inv = __uint_as_float((uint32_t)(254 - ev) << 23);
+  int ev[NI];
+  node_exponents<D>(x, 8, 127 - 60, ev);  // (see v_scale_used)
 #pragma unroll
-  for (int i = 0; i < NI; ++i)
+  for (int i = 0; i < NI; ++i) {
+    const int r = 16 * grp + i * RPI + r_in;
+    const float inv = __uint_as_float((uint32_t)(254 - ev[i]) << 23);
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const uint32_t w[4] = {x[2 * i + k].x, x[2 * i + k].y, x[2 * i + k].z, x[2 * i + k].w};
       uint32_t h[4];
 #pragma unroll
       for (int c = 0; c < 4; ++c) h[c] = scaled_f16(w[c], inv);
-      *reinterpret_cast<uint4*>(v16 + sw128_chunk_off(16 * grp + i * RPI + r_in, 2 * ch + k, TC_BN)) = make_uint4(h[0], h[1], h[2], h[3]);
+      *reinterpret_cast<uint4*>(v16 + sw128_chunk_off(r, 2 * ch + k, TC_BN)) = make_uint4(h[0], h[1], h[2], h[3]);
     }
-  if (lane == 0) {
-    ring.lsv[grp] = (float)(ev - 127);
-    ring.isv[grp] = __uint_as_float((uint32_t)(254 - ev) << 23);
+    if (ch == 0) scales.log_v[r] = (float)(ev[i] - 127);
   }
 }
 template <int D>
-__device__ inline void put_node_k(int grp, int lane, const uint4 (&y)[D / 16], uint8_t* k1, uint8_t* k2, ScaleRing ring) {
+__device__ inline void put_node_k(int grp, int lane, const uint4 (&y)[D / 16], uint8_t* k1, uint8_t* k2, NodeScales scales) {
   constexpr int RPI = 512 / D, NI = 16 / RPI;
   const int ch = lane_chunk<D>(lane), r_in = lane_row<D>(lane);
-  const int ek = node_exponent(y, 7, 1);
-  const float inv = __uint_as_float((uint32_t)(254 - ek) << 23);
+  int ek[NI];
+  node_exponents<D>(y, 7, 1, ek);
 #pragma unroll
   for (int i = 0; i < NI; ++i) {
+    const int r = 16 * grp + i * RPI + r_in;
+    const float inv = __uint_as_float((uint32_t)(254 - ek[i]) << 23);
     uint32_t hi[4], lo[4];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
@@ -272,11 +291,61 @@ __device__ inline void put_node_k(int grp, int lane, const uint4 (&y)[D / 16], u
         lo[2 * k + c] = l0 | ((uint32_t)l1 << 16);
       }
     }
-    const uint32_t off = code_tile_off<D>(16 * grp + i * RPI + r_in, ch);
+    const uint32_t off = code_tile_off<D>(r, ch);
     *reinterpret_cast<uint4*>(k1 + off) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
     *reinterpret_cast<uint4*>(k2 + off) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    if (ch == 0) scales.k[r] = __uint_as_float((uint32_t)ek[i] << 23);
   }
-  if (lane == 0) ring.ks[grp] = __uint_as_float((uint32_t)ek << 23);
+}
+
+// A row's step over the tree: 64 scores of nodes, of which those count whose bit of `words` is set, become probabilities.  A node's
+// exponent is its score times the scales of Q and K, plus the logarithm of V's power of two; the reference is the largest of them.
+// scales: shared address of the nodes' K scales, SB_MAX_NODES floats before the logarithms.  -> reference (-inf: no node is visible),
+// denominator relative to it.  The denominator is summed on its own, from scores: the columns have no common V scale.
+__device__ __forceinline__ float2 tree_step(uint32_t addr, uint2 words, float qs, uint32_t scales) {
+  float most = -INFINITY, ref = -INFINITY, sum = 0.f;
+  if (!__any_sync(0xffffffffu, (words.x | words.y) != 0)) {
+    const uint32_t none[16] = {};
+    tmem_st16(addr, none);
+    tmem_st16(addr + 16, none);
+    return make_float2(ref, sum);
+  }
+#pragma unroll 1
+  for (int pass = 0; pass < 4; ++pass) {  // both halves for the largest, both for the probabilities (stored over scores that are done with)
+    const int q = pass & 1;
+    const uint32_t word = q ? words.y : words.x, at = scales + q * 128;
+    uint32_t x[32];
+    tmem_ld32(addr + 32 * q, x);
+    float s[32], d[32];
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {
+      const float4 k = lds_float4(at + e * 4), v = lds_float4(at + (SB_MAX_NODES + e) * 4);
+      const float f[4] = {qs * k.x, qs * k.y, qs * k.z, qs * k.w}, lv[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const bool on = (word >> (e + c)) & 1u;
+        s[e + c] = on ? __uint_as_float(x[e + c]) * f[c] : -INFINITY;
+        d[e + c] = on ? s[e + c] + lv[c] : -INFINITY;
+      }
+    }
+    if (pass < 2) {
+#pragma unroll
+      for (int e = 0; e < 32; e += 2) {
+        most = max3(most, s[e], s[e + 1]);
+        ref = max3(ref, d[e], d[e + 1]);
+      }
+    } else {
+      const float m = most == -INFINITY ? 0.f : most, r = ref == -INFINITY ? 0.f : ref;
+      uint32_t pk[16];
+#pragma unroll
+      for (int e = 0; e < 32; e += 2) {
+        sum += fast_exp2(s[e] - m) + fast_exp2(s[e + 1] - m);
+        pk[e >> 1] = pack_f16(fast_exp2(d[e] - r), fast_exp2(d[e + 1] - r));
+      }
+      tmem_st16(addr + 16 * q, pk);
+    }
+  }
+  return make_float2(ref, ref == -INFINITY ? sum : sum * fast_exp2(most - ref));
 }
 
 // Scores of 32 columns whose bit is not set become -inf.
@@ -351,11 +420,13 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   int* s_err = reinterpret_cast<int*>(base + 3340);
   uint32_t* s_bad = reinterpret_cast<uint32_t*>(base + 3344);        // [4]: node rows with a NaN or an infinity
   uint32_t* s_flag = reinterpret_cast<uint32_t*>(base + 3360);       // [8 slots]: bits 0-7 the groups with a NaN scale, bits 8-15 those whose V reads as zeros
+  // Eight slots: the loader writes block j's when S of block j - 3 is done, i.e. the softmax with block j - 5.
   float* s_ks = reinterpret_cast<float*>(base + 7168);               // [8 slots][8 groups of 16 keys] K scale
   float* s_lsv = s_ks + 64;                                          // log2 of the V scale
   float* s_isv = s_lsv + 64;                                         // 1 / V scale
   float* s_qs = reinterpret_cast<float*>(base + 3840);               // [128 rows] scale of a Q row
   float* s_ml = reinterpret_cast<float*>(base + 4864);               // [2 streams][reference, sum][128 rows]
+  float* s_node = s_ml;                                              // [2][128 nodes]: NodeScales; read before the first P V, s_ml written after the last
   uint8_t* sQ = base + QT_SMALL;      // [2 terms]
   uint8_t* sK = sQ + 2 * TILE8;       // [3 stages] codes
   uint8_t* sK2 = sK + 3 * TILE8;      // second term of the tree's K
@@ -439,7 +510,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     }
     // Nodes: warp w takes V (w even) or K (odd) of groups w / 2 and 4 + w / 2 of 16 nodes.  (Rolled: this code runs once, and costs its
     // instruction fetches: unrolled twice 16 trees take 134.5 us, so 133.2.)
-    const ScaleRing ring = {s_ks, s_lsv, s_isv};
+    const NodeScales scales = {s_node, s_node + SB_MAX_NODES};
 #pragma unroll 1
     for (int grp = warp >> 1; grp < groups; grp += 4) {
       uint4 xn[D / 16];
@@ -447,16 +518,12 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
                         grp, lane, xn);
       const uint32_t bits = drop_bad_rows<D>(lane, xn);
       if (bits && lane == 0) atomicOr(&s_bad[grp >> 1], bits << (16 * (grp & 1)));
-      if (warp & 1) put_node_k<D>(grp, lane, xn, sK, sK2, ring);
-      else put_node_v<D>(grp, lane, xn, sV, ring);
+      if (warp & 1) put_node_k<D>(grp, lane, xn, sK, sK2, scales);
+      else put_node_v<D>(grp, lane, xn, sV, scales);
     }
     if (tree_blocks) {  // groups without nodes: K may be anything (masked), V has to be finite
       for (int i = groups * 2 * D + tid; i < TC_BN * D / 8; i += QT_SOFTMAX)
         *reinterpret_cast<uint4*>(sV + sw128_chunk_off(i / (D / 8), i % (D / 8), TC_BN)) = make_uint4(0, 0, 0, 0);
-      if (tid >= groups && tid < 8) {
-        s_ks[tid] = s_isv[tid] = 1.f;
-        s_lsv[tid] = 0.f;
-      }
     }
 #pragma unroll
     for (int i = 0; i < NQ; ++i) {
@@ -582,48 +649,63 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       tmem_st16(s_addr, pk[0]);
       tmem_st16(s_addr + 16, pk[1]);
     };
-    // A wait that gives up leaves `ok` false; the loop still runs to its end, so that every barrier gets its arrivals.
-    for (int i = 0; i < nb; ++i) {
-      const int group = (i & 7) * 8 + t_mine * 4;
-      const bool is_tree = i < tree_blocks;
-      const int k0 = (is_tree ? 0 : prefix_key(i)) + 64 * t_mine;
-      // steps that every row sees whole need no mask
-      const bool masked = is_tree || k0 + 64 > si.P || (p.window > 0 && k0 + 64 > p.sinks && si.P + si.n - 1 - k0 >= p.window);
+    // A wait that gives up leaves `ok` false; the steps still run to their end, so that every barrier gets its arrivals.
+    auto await_scores = [&](int i) {
       if (ok) ok = mbar_wait(&s_bar[QB_SC0 + (i & 7)], (i >> 3) & 1, s_abort) &&
                    mbar_wait(&s_bar[QB_S_FULL0 + (i & 1)], (i >> 1) & 1, s_abort);
       __syncwarp();
       tc_fence_after();
-      const uint32_t s_addr = tmem + lane_base + (2 * (i & 1) + t_mine) * 64;
-      const uint32_t flags = is_tree ? 0u : (s_flag[i & 7] >> (4 * t_mine)) & 15u;   // poisoned 16-key groups of the step
-      if (masked || flags) {
-        // invisible scores become -inf in tensor memory before the walk
-#pragma unroll 1
-        for (int q = 0; q < 2; ++q) {
-          uint32_t word;
-          if (is_tree) {
-            const int w0 = (k0 >> 5) + q;    // k0: first node of the step
-            word = node >= 0 ? s_anc[4 * node + w0] : 0u;
-            if (p.window > 0 && p.window < si.n) {  // (a node's ancestors lie less than n positions back)
-              for (uint32_t w = word; w; w &= w - 1) {
-                const int bit = __ffs(w) - 1, kp = si.P + s_depth[32 * w0 + bit];
-                if (!(kp < p.sinks || pos - kp < p.window)) word &= ~(1u << bit);
-              }
-            }
-            poison |= (word & s_bad[w0]) != 0;
-          } else {
-            const int kq = k0 + 32 * q;
-            word = low_bits(si.P - kq);
-            if (p.window > 0) word &= low_bits(p.sinks - kq) | ~low_bits(pos - p.window + 1 - kq);
-            poison |= ((flags >> (2 * q)) & 1u && (word & 0xFFFFu)) || ((flags >> (2 * q + 1)) & 1u && (word >> 16));
-          }
-          if (__any_sync(0xffffffffu, word != ~0u)) mask_scores(s_addr + 32 * q, word);
-        }
-      }
-      walk(i, group, s_addr);
+      return tmem + lane_base + (2 * (i & 1) + t_mine) * 64;
+    };
+    auto hand_over = [&](int i) {
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&s_bar[QB_P_FULL0 + (i & 1)]);
+    };
+    if (tree_blocks) {
+      const uint32_t s_addr = await_scores(0);
+      uint2 words = make_uint2(0u, 0u);
+#pragma unroll 1
+      for (int q = 0; q < 2; ++q) {
+        const int w0 = 2 * t_mine + q;         // the nodes 32 w0 .. + 31
+        uint32_t word = node >= 0 ? s_anc[4 * node + w0] : 0u;
+        if (p.window > 0 && p.window < si.n) {  // (a node's ancestors lie less than n positions back)
+          for (uint32_t w = word; w; w &= w - 1) {
+            const int bit = __ffs(w) - 1, kp = si.P + s_depth[32 * w0 + bit];
+            if (!(kp < p.sinks || pos - kp < p.window)) word &= ~(1u << bit);
+          }
+        }
+        poison |= (word & s_bad[w0]) != 0;
+        if (q) words.y = word;
+        else words.x = word;
+      }
+      const float2 r = tree_step(s_addr, words, qs, smem_u32(s_node + 64 * t_mine));
+      seen_any = r.x > -INFINITY;
+      if (seen_any) ref = r.x;
+      l_run = r.y;
+      hand_over(0);
+    }
+    for (int i = tree_blocks; i < nb; ++i) {
+      const int group = (i & 7) * 8 + t_mine * 4;
+      const int k0 = prefix_key(i) + 64 * t_mine;
+      // steps that every row sees whole need no mask
+      const bool masked = k0 + 64 > si.P || (p.window > 0 && k0 + 64 > p.sinks && si.P + si.n - 1 - k0 >= p.window);
+      const uint32_t s_addr = await_scores(i);
+      const uint32_t flags = (s_flag[i & 7] >> (4 * t_mine)) & 15u;   // poisoned 16-key groups of the step
+      if (masked || flags) {
+        // invisible scores become -inf in tensor memory before the walk
+#pragma unroll 1
+        for (int q = 0; q < 2; ++q) {
+          const int kq = k0 + 32 * q;
+          uint32_t word = low_bits(si.P - kq);
+          if (p.window > 0) word &= low_bits(p.sinks - kq) | ~low_bits(pos - p.window + 1 - kq);
+          poison |= ((flags >> (2 * q)) & 1u && (word & 0xFFFFu)) || ((flags >> (2 * q + 1)) & 1u && (word >> 16));
+          if (__any_sync(0xffffffffu, word != ~0u)) mask_scores(s_addr + 32 * q, word);
+        }
+      }
+      walk(i, group, s_addr);
+      hand_over(i);
     }
     if (!ok) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
     if (poison) l_run = __uint_as_float(0x7FC00000u);

@@ -96,3 +96,26 @@ def test_attention_nan_codes_before_the_window_do_not_matter(batch, H, G, n, D, 
     out, lse, status = sb.sb_tree_attention_quant(cache.gpu(sb), tree_of(P, parents, q.shape[1]), q.cuda(), k.cuda(), v.cuda(), window=window, sinks=sinks)
     assert status.tolist() == [0] * batch
     assert torch.equal(out, want) and torch.equal(lse, wlse)
+
+
+@pytest.mark.parametrize("batch,H,G,n", KERNELS)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("log_f", [6, 12, 16, 40, 100])
+@pytest.mark.parametrize("which", ["k", "v", "both"])
+def test_attention_large_finite_nodes_change_only_the_nodes_that_see_them(batch, H, G, n, D, log_f, which):
+    """Leaves 2^log_f times larger than the other nodes.  Nobody but a leaf itself sees it: the others' results stay as they
+    are with ordinary leaves, within the bound that counts their visible keys alone."""
+    P = [[300, 0, 77, 513][b % 4] for b in range(batch)]
+    cache, parents, q, k, v = make(72, P, [n] * batch, H=H, G=G, D=D)
+    large = np.zeros(q.shape[0], bool)
+    for b in range(batch):
+        leaves = [i for i in range(n) if i not in parents[b]]
+        large[[b * n + i for i in leaves[::2]]] = True
+    f = torch.from_numpy(np.where(large, 2.0 ** log_f, 1.0)).float()[:, None, None]
+    k2 = (k.float() * f).bfloat16() if which != "v" else k
+    v2 = (v.float() * f).bfloat16() if which != "k" else v
+    out, lse = check(cache, P, parents, q, k2, v2)
+    if H == 8:      # the tcgen05 kernel keeps a row's arithmetic to itself: not a bit changes
+        want, wlse = check(cache, P, parents, q, k, v)
+        others = torch.from_numpy(~large).cuda()
+        assert torch.equal(out[others], want[others]) and torch.equal(lse[others], wlse[others])
