@@ -119,3 +119,73 @@ def test_attention_large_finite_nodes_change_only_the_nodes_that_see_them(batch,
         want, wlse = check(cache, P, parents, q, k, v)
         others = torch.from_numpy(~large).cuda()
         assert torch.equal(out[others], want[others]) and torch.equal(lse[others], wlse[others])
+
+
+@pytest.mark.parametrize("batch,H,G,n", KERNELS)
+@pytest.mark.parametrize("log_gap", [6, 12])
+def test_attention_blocks_of_small_scale_count_beside_large_ones(batch, H, G, n, log_gap):
+    """Every second block has a V scale 2^log_gap times the others' and codes of nought, so that the result is the share of the
+    small blocks alone.  A probability times its V scale is off by 2^-11 of itself or, below fp16's normal range, by 2^-25 of the largest
+    probability times the largest scale; half the outputs' last bit comes on top."""
+    P = [[320, 160, 64, 512][b % 4] for b in range(batch)]
+    D = 64
+    cache, parents, q, k, v = make(75, P, [n] * batch, H=H, G=G, D=D, block=16, page_size=16)
+    cache.scales[1][:] = 2.0 ** -8
+    for b in range(batch):
+        for j in range(0, P[b], 32):
+            r = cache.row(b, j)
+            cache.scales[1][0, r // 16] = 2.0 ** (log_gap - 8)
+            cache.codes[1][0, r:r + 16] = 0
+    v = (v.float() * 0).bfloat16()
+    out, lse, status = sb.sb_tree_attention_quant(cache.gpu(sb), tree_of(P, parents, H * G), q.cuda(), k.cuda(), v.cuda())
+    assert status.tolist() == [0] * batch
+    out = out.double().cpu().numpy()
+    for b in range(batch):
+        rows = [cache.row(b, j) for j in range(P[b])]
+        kk, vv = cache.values(0, 0, b, P[b]), cache.values(1, 0, b, P[b])
+        scale_v = cache.scales[1][0, np.asarray(rows) // 16]
+        for i in range(n):
+            at = b * n + i
+            seen = qh.chain(parents[b], i)
+            for h in range(H * G):
+                qq = q[at, h].double().numpy() / np.sqrt(D)
+                s = np.concatenate([kk[:, h // G] @ qq, k[[b * n + a for a in seen], h // G].double().numpy() @ qq])
+                p = np.exp(s - s.max())
+                weight = np.abs(vv[:, h // G] / scale_v[:, h // G, None])
+                # scores: fp32 sums of exact products, with Q to 2^-18 of its row's largest element
+                ds = 2.0 ** -18 * (np.abs(kk[:, h // G]).sum(1).max() * np.abs(qq).max())
+                per = p[:P[b]] * scale_v[:, h // G]
+                tol = (np.maximum(per * 2.0 ** -11, 2.0 ** -25 * p.max() * scale_v[:, h // G].max()) + 2 * ds * per) @ weight / p.sum()
+                exact = p[:P[b]] @ vv[:, h // G] / p.sum()
+                assert (np.abs(out[at, h] - exact) <= tol + np.abs(exact) * (2.0 ** -8 + 2 * ds) + 1e-30).all()
+
+
+def test_attention_every_status_of_malformed_offsets():
+    P, N = [64] * 6, [40] * 6
+    cache, parents, q, k, v = make(65, P, N, H=8, G=2)
+    want, wlse, _ = sb.sb_tree_attention_quant(cache.gpu(sb), tree_of(P, parents, 16), q.cuda(), k.cuda(), v.cuda())
+    offsets = [0, 40, 100, 90, 130, 170, 100000]      # 40 nodes; 60, more than announced; -10; 40 and 40 across the trees; past the rows
+    tree = tree_of(P, parents, 16, node_offsets=i32(offsets), max_nodes=45)
+    all_parents = [p for t in parents for p in t]
+    assert any(p >= i for i, p in enumerate(all_parents[90:130])) and any(p >= i for i, p in enumerate(all_parents[130:170]))
+    out, lse = torch.full_like(want, 3.0), torch.full_like(wlse, 3.0)
+    _, _, st = sb.sb_tree_attention_quant(cache.gpu(sb), tree, q.cuda(), k.cuda(), v.cuda(), out=out, lse=lse)
+    assert st.tolist() == [0, 4, 4, 4, 4, 4]
+    assert torch.equal(out[:40], want[:40]) and torch.equal(lse[:40], wlse[:40])
+    assert (out[40:90] == 3.0).all() and (lse[40:90] == 3.0).all()        # nobody's rows
+    assert not out[90:170].any() and not lse[90:170].any()                # rows of sequences 3 and 4, whose trees are none
+    assert (out[170:] == 3.0).all() and (lse[170:] == 3.0).all()
+
+
+@pytest.mark.parametrize("P,N,H", [([40, 0], [1, 2], 2), ([300, 100], [90, 33], 8)])
+@pytest.mark.parametrize("num_splits", [0, 11])
+def test_attention_serves_its_rows_beside_others_with_any_number_of_chunks(P, N, H, num_splits):
+    cache, parents, q, k, v = make(70, P, N, H=H, G=2)
+    total = q.shape[0]
+    want, wlse = check(cache, P, parents, q, k, v, num_splits=num_splits)
+    more = torch.cat([q, q[:5]]).cuda()
+    out, lse = torch.full_like(more, 3.0), torch.full(more.shape[:2], 3.0, device="cuda")
+    sb.sb_tree_attention_quant(cache.gpu(sb), tree_of(P, parents, 2 * H), more, k.cuda(), v.cuda(), out=out, lse=lse, num_splits=num_splits,
+                               q_offsets=i32([0, N[0]]))
+    assert (out[total:] == 3.0).all() and (lse[total:] == 3.0).all()
+    assert torch.equal(out[:total], want) and torch.equal(lse[:total], wlse)
