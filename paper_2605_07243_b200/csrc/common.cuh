@@ -82,6 +82,19 @@ struct PerDeviceInt {
   }
 };
 
+// SMs of the current device (148 where it cannot be asked).
+inline int device_sms() {
+  static PerDeviceInt cache;
+  return cache.get([]() {
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) {
+      cudaGetLastError();
+      sms = 148;
+    }
+    return sms;
+  }, 148);
+}
+
 // Programmatic dependent launch.  A kernel started with launch_dependent() may begin while its
 // predecessor in the stream is still running; it must execute pdl_wait() before it reads anything
 // the predecessor writes (and always before it ends, so that completion stays transitive along

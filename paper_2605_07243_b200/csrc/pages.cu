@@ -587,7 +587,7 @@ extern "C" sb_status sb_pages_copy(const sb_page_array* arrays, int32_t n_arrays
   if (max_copies == 0) return SB_OK;
   // four CTAs per SM when the list could be long enough to fill them
   const long long most = (long long)max_copies * n_layers * pieces;
-  const int grid = (int)(most < 148 * 4 ? most : 148 * 4);
+  const int fill = 4 * device_sms(), grid = (int)(most < fill ? most : fill);
   return launch_dependent(pages_copy_kernel, dim3(grid), dim3(PC_THREADS), static_cast<cudaStream_t>(stream), arr, n_layers,
                           num_pages, copy_src, copy_dst, n_copies, max_copies);
 }

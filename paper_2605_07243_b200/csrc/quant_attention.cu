@@ -52,19 +52,6 @@ __global__ void __launch_bounds__(256) quant_merge_kernel(const QuantAttnParams 
   if (p.lse && col == 0) p.lse[grow] = sum == 0.f ? 0.f : (M + log2f(sum)) * kLn2;
 }
 
-static int quant_num_sms() {
-  static PerDeviceInt cache;
-  return cache.get([]() {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || sms <= 0) {
-      cudaGetLastError();
-      sms = 148;
-    }
-    return sms;
-  }, 148);
-}
-
 struct QuantPlan {
   bool tc;                         // the tcgen05 kernel; else the 16-row kernel
   int cluster, outer, grid_tiles;  // grid_tiles: row tiles (16 or 128 rows) per KV head
@@ -77,7 +64,7 @@ static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree,
   const int rows = (nq > 0 ? nq : 1) * G;
   long long keys = tree->max_prefix;  // visible ones, at most
   if (window > 0 && (long long)window + sinks + 64 < keys) keys = (long long)window + sinks + 64;
-  const int sms = quant_num_sms();
+  const int sms = device_sms();
   // The 16-row kernel starts and ends in less time (9 us against 12), but walks the keys once per 16 rows, with the slower matrix
   // instructions.  us by it and by the tcgen05 kernel, 8 KV heads, groups of 4: 1 to 4 nodes (one tile), 2k keys 11.7 / 18.6, 64 ragged 8k
   // prefixes 143 / 199; 16 nodes over 128, 512, 2k keys 10 / 12, 11 / 15, 14 / 18; 32 nodes 11 / 12, 13 / 15, 19 / 18.5; 60 nodes
@@ -241,9 +228,9 @@ extern "C" sb_status sb_tree_attention_quant(const sb_quant_cache* kv, int32_t l
   const dim3 grid(p.num_splits, pl.grid_tiles * kv->n_kv_heads, kv->batch);
   if (grid.y > 65535) return SB_ERR_UNSUPPORTED;
   p.sort_seqs = kv->batch > 1 && kv->batch <= SB_MAX_NODES &&
-                (long long)grid.x * grid.y * grid.z > (pl.tc ? 1LL : 2LL) * quant_num_sms() ? 1 : 0;
+                (long long)grid.x * grid.y * grid.z > (pl.tc ? 1LL : 2LL) * device_sms() ? 1 : 0;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  const sb_status ls = pl.tc ? launch_quant_tc(p, grid, cs) : launch_quant_rows(p, grid, pl.cluster, cs);
+  const sb_status ls = pl.tc ? launch_quant_tc(p, grid, cs) : launch_quant_rows(p, grid, pl.cluster, device_sms(), cs);
   if (ls != SB_OK || pl.outer == 1) return ls;
   const int rows_max = tree->max_nodes * tree->n_q_heads;
   auto merge = [&](auto kernel, int rows_per_cta) {

@@ -167,7 +167,7 @@ inline sb_status make_code_maps(const QuantAttnParams& p, int most, CUtensorMap*
 template <int D>
 constexpr int kPartRow = 2 * D + 16;
 constexpr int kQuantMaxCluster = 8;
-sb_status launch_quant_rows(const QuantAttnParams& p, dim3 grid, int cluster, cudaStream_t cs);
+sb_status launch_quant_rows(const QuantAttnParams& p, dim3 grid, int cluster, int sms, cudaStream_t cs);
 sb_status launch_quant_tc(const QuantAttnParams& p, dim3 grid, cudaStream_t cs);
 
 }  // namespace sb

@@ -637,7 +637,7 @@ __global__ void __launch_bounds__(QR_THREADS, 3) quant_rows_kernel(const QuantAt
 }
 
 template <int D>
-static sb_status launch_rows(const QuantAttnParams& p, dim3 grid, int cluster, cudaStream_t cs) {
+static sb_status launch_rows(const QuantAttnParams& p, dim3 grid, int cluster, int sms, cudaStream_t cs) {
   static PerDeviceOnce once;
   if (!once.run([]() {
         const bool ok = cudaFuncSetAttribute(quant_rows_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
@@ -651,7 +651,7 @@ static sb_status launch_rows(const QuantAttnParams& p, dim3 grid, int cluster, c
   cfg.gridDim = grid;
   cfg.blockDim = dim3(QR_THREADS);
   // a merge buffer of its own costs the third CTA of an SM: only where two to an SM are enough
-  const int merge_apart = cluster > 1 && (long long)grid.x * grid.y * grid.z <= 2LL * 148 ? 1 : 0;
+  const int merge_apart = cluster > 1 && (long long)grid.x * grid.y * grid.z <= 2LL * sms ? 1 : 0;
   cfg.dynamicSmemBytes = merge_apart ? QrLayout<D>::BYTES_APART : QrLayout<D>::BYTES_OVER;
   cfg.stream = cs;
   cudaLaunchAttribute attr[2];
@@ -674,8 +674,8 @@ static sb_status launch_rows(const QuantAttnParams& p, dim3 grid, int cluster, c
   return launch_check();
 }
 
-sb_status launch_quant_rows(const QuantAttnParams& p, dim3 grid, int cluster, cudaStream_t cs) {
-  return p.kv.head_dim == 64 ? launch_rows<64>(p, grid, cluster, cs) : launch_rows<128>(p, grid, cluster, cs);
+sb_status launch_quant_rows(const QuantAttnParams& p, dim3 grid, int cluster, int sms, cudaStream_t cs) {
+  return p.kv.head_dim == 64 ? launch_rows<64>(p, grid, cluster, sms, cs) : launch_rows<128>(p, grid, cluster, sms, cs);
 }
 
 }  // namespace sb

@@ -1,4 +1,7 @@
 """Host side of the calls over 8-bit caches and pages: calls whose tensors the library cannot be told of.  No GPU."""
+import re
+from pathlib import Path
+
 import pytest
 import torch
 
@@ -25,3 +28,12 @@ def test_strided_rows_of_other_dimensions_are_refused():
     with pytest.raises(ValueError, match="dimensions"):
         sb._rows_of(fused[:, :, 3:5], 2, 64, -1, "rows")
     assert sb._rows_of(fused, 7, 64, -1, "rows") == (fused.data_ptr(), 7 * 64)
+
+
+def test_the_number_of_sms_is_asked_for_in_one_place():
+    """The planner of the 8-bit attention, the choice of its merge buffer and the grid of the page copies go by the same device."""
+    csrc = Path(sb.__file__).parent / "csrc"
+    for name in ("quant_attention.cu", "quant_attention_rows.cu", "quant_attention_tc.cu", "kv_append_quant.cu", "pages.cu"):
+        code = re.sub(r"//[^\n]*", "", (csrc / name).read_text())
+        assert not re.search(r"\b148\b", code), name
+    assert "device_sms()" in (csrc / "pages.cu").read_text() and "device_sms()" in (csrc / "quant_attention.cu").read_text()
