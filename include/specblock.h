@@ -469,7 +469,8 @@ sb_status sb_path_rows(int32_t batch, const int32_t* node_offsets, const int32_t
  *   codes  : page_size == 0  [batch][kv_capacity][n_kv_heads][head_dim], kv_capacity a multiple of scale_block
  *            page_size  > 0  [num_pages][page_size][n_kv_heads][head_dim], page_size a multiple of scale_block
  *   scales : [tokens of the cache / scale_block][n_kv_heads], the blocks in the order of the codes' rows
- *   n_layers layers, codes_layer_stride elements and scale_layer_stride scales apart.
+ *   n_layers layers, codes_layer_stride elements and scale_layer_stride scales apart (sb_kv_append_quant, which writes all of
+ *   them, refuses layers that overlap).
  * sb_kv_append_quant writes powers of two; the attention takes any positive scale up to 2^40.  A V scale
  * below 2^-60 reads as a block of zeros; a NaN scale marks a block that was written from a NaN or an infinity:
  * every node that sees one of its tokens gets NaN.  Codes are finite (0x7F and 0xFF, e4m3's NaN, are
@@ -575,8 +576,8 @@ sb_status sb_kv_append_quant(const sb_quant_cache* kv, const void* k_rows, const
  *   - `slots` and the other lists hold n >= 0 int32 entries (host count n); status int32 [n], per entry.  An
  *     entry with a slot outside [0, n_slots), or a slot that an earlier entry of the list names, gets
  *     SB_ERR_INVALID_ARG; an entry whose table is damaged (held > max_pages, a page id outside the pool, a page
- *     with refs < 1) or whose lengths do not fit gets SB_ERR_BOUNDS.  Such an entry changes nothing; the others
- *     are served.
+ *     with refs < 1; looked for in the pages that the call shares, makes writable or lets go, sb_pages_compact: in all) or whose
+ *     lengths do not fit gets SB_ERR_BOUNDS.  Such an entry changes nothing; the others are served.
  *   - workspace: sb_pages_workspace_bytes(pool, n) bytes, 256-byte aligned, no initialisation.
  *   - calls on one pool are ordered by the caller's stream.
  */

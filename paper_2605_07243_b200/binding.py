@@ -790,7 +790,7 @@ class PagePool:
 @dataclass(frozen=True)
 class PageCopies:
     """The (source, destination) page pairs that sb_pages_reserve / sb_pages_compact leave for sb_pages_copy: src, dst
-    int32 [room], -1 behind the count[0] pairs."""
+    int32 [room], the pairs first, count[0] of them; then -1, after sb_pages_reserve up to the length of its list."""
     src: torch.Tensor
     dst: torch.Tensor
     count: torch.Tensor

@@ -259,6 +259,10 @@ extern "C" sb_status sb_kv_append_quant(const sb_quant_cache* kv, const void* k_
   if (row_stride == 0) row_stride = width;
   if (row_stride < width || row_stride % 8 != 0 || rows_layer_stride < 0 || rows_layer_stride % 8 != 0) return SB_ERR_INVALID_ARG;
   if ((reinterpret_cast<uintptr_t>(k_rows) & 15) || (reinterpret_cast<uintptr_t>(v_rows) & 15)) return SB_ERR_INVALID_ARG;
+  // layers that overlap would be written by several CTAs at once
+  if (kv->n_layers > 1 && (kv->codes_layer_stride < quant_rows_total(*kv) * width ||
+                           kv->scale_layer_stride < quant_rows_total(*kv) / kv->scale_block * kv->n_kv_heads))
+    return SB_ERR_INVALID_ARG;
   AppendParams p;
   p.kv = *kv;
   p.rows[0] = static_cast<const uint16_t*>(k_rows);

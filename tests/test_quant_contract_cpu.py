@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from paper_2605_07243_b200 import binding as sb
+from test_quant_cpu import INVALID, append, cache
 
 
 def test_rows_that_overlap_are_refused():
@@ -28,6 +29,15 @@ def test_strided_rows_of_other_dimensions_are_refused():
     with pytest.raises(ValueError, match="dimensions"):
         sb._rows_of(fused[:, :, 3:5], 2, 64, -1, "rows")
     assert sb._rows_of(fused, 7, 64, -1, "rows") == (fused.data_ptr(), 7 * 64)
+
+
+@pytest.mark.parametrize("page_size", [0, 16])
+def test_append_refuses_layers_that_overlap(page_size):
+    """8 pages (or 2 sequences) of 16 tokens, 2 heads of 64: a layer has 16384 (4096) codes and 16 (4) scales."""
+    codes, scales = (16384, 16) if page_size else (4096, 4)
+    for n_layers, code_stride, scale_stride in ((2, codes - 16, scales), (2, codes, scales - 1), (3, 0, scales), (2, codes, 0)):
+        kv = cache(n_layers=n_layers, codes_layer_stride=code_stride, scale_layer_stride=scale_stride, page_size=page_size, kv_capacity=16)
+        assert append(kv=kv) == INVALID
 
 
 def test_the_number_of_sms_is_asked_for_in_one_place():
