@@ -68,7 +68,8 @@ static QuantPlan plan_quant(const sb_quant_cache* kv, const sb_quant_tree* tree,
   // The 16-row kernel starts and ends in less time (9 us against 12), but walks the keys once per 16 rows, with the slower matrix
   // instructions.  us by it and by the tcgen05 kernel, 8 KV heads, groups of 4: 1 to 4 nodes (one tile), 2k keys 11.7 / 18.6, 64 ragged 8k
   // prefixes 143 / 199; 16 nodes over 128, 512, 2k keys 10 / 12, 11 / 15, 14 / 18; 32 nodes 11 / 12, 13 / 15, 19 / 18.5; 60 nodes
-  // 13 / 13, 17 / 16, 29 / 20; 8 nodes, 4 ragged 8k prefixes 37 / 34, 16 of them 84 / 70, 64 of them 232 / 199.
+  // 13 / 13, 17 / 16, 29 / 20; 8 nodes, 4 ragged 8k prefixes 37 / 34, 16 of them 84 / 70, 64 of them 232 / 199.  (These and the counts of chunks
+  // below were measured with D = 128 and that head layout; others go by the same numbers.)
   const long long tiles = (long long)kv->batch * kv->n_kv_heads * ceil_div(rows, 16);
   pl.tc = rows > 16 && (tiles > 64 || tiles * keys > (1 << 17));
   pl.cluster = 1;

@@ -19,7 +19,7 @@
 // one buffer per stream the warps spent half of their time waiting for PV and S of their own stream.
 // (One tile per CTA, although two tiles could share a key block's loads and conversions: both are off the critical path, which
 // is the exponentials, and the smaller units fill the SMs more evenly: 191 us against 150 on 16 ragged trees,
-// which take 132 now.)
+// which take 131 now.)
 //
 // The softmax thread does not compute a maximum after its row's first visible key: the reference is raised when the sum of 64
 // probabilities shows that an exponent is far above it (P' is fp16, which ends at 2^16), a rare event that
@@ -563,7 +563,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
     bool poison = false;
 
     // One step's 64 scores of this row -> probabilities.  The two halves have no branch between them, so that one fills the
-    // gaps of the other (a check of the reference after each half: 16 trees 148 us, long trees 686; one check: 136 and 645).
+    // gaps of the other (a check of the reference after each half: 16 trees 148 us; one check: 136).
     auto walk = [&](int i, int group, uint32_t s_addr) {
       const float4 ks = *reinterpret_cast<const float4*>(s_ks + group), ls = *reinterpret_cast<const float4*>(s_lsv + group);
       const float4 is = *reinterpret_cast<const float4*>(s_isv + group);
@@ -586,7 +586,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
           // some exponentials go to the FMA pipe: the other pipe does 16 a clock (of 64 columns 4 / 8 / 12 / 16: 134 / 136 / 136 / 138
-          // us on 16 trees, 644 / 645 / 648 / 658 on long ones)
+          // us on 16 trees; on long ones 12 and 16 take 0.5 and 2 % longer than 8)
           float p0, p1;
           const float d0 = d[32 * h + e], d1 = d[32 * h + e + 1];
           if ((e & 15) == 14) {
