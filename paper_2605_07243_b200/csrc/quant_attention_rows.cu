@@ -126,7 +126,7 @@ __global__ void __launch_bounds__(QR_THREADS, 3) quant_rows_kernel(const QuantAt
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
   __shared__ uint64_t s_full[QR_WARPS][QR_STAGES];
-  __shared__ int s_abort;
+  __shared__ int s_abort, s_late;                    // a wait gave up; the same for the waits after that
   __shared__ int s_page[QR_WARPS][4][2];             // ids of the pages of the two halves of coming groups
   __shared__ __align__(16) int s_parent[SB_MAX_NODES];
   __shared__ uint32_t s_anc[SB_MAX_NODES * 4];
@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(QR_THREADS, 3) quant_rows_kernel(const QuantAt
   if (tid == 0) {
     asm volatile("prefetch.tensormap [%0];" ::"l"(&kmap));
     asm volatile("prefetch.tensormap [%0];" ::"l"(&vmap));
-    s_abort = 0;
+    s_abort = s_late = 0;
     for (int i = 0; i < QR_WARPS * QR_STAGES; ++i) mbar_init(&s_full[0][0] + i, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -517,7 +517,11 @@ __global__ void __launch_bounds__(QR_THREADS, 3) quant_rows_kernel(const QuantAt
         mma_f16(o[4 * k + 3], pa, half2_of_e4m3x2((uint16_t)(lo1 >> 16)), half2_of_e4m3x2((uint16_t)(hi1 >> 16)));
       }
     }
-    __syncwarp();
+    ok = __all_sync(0xffffffffu, ok);
+    if (!ok) {  // nothing more is asked for; what is in flight is awaited, again with a limit, before shared memory has another use
+      for (int k = i; k < min(i + QR_STAGES, codes_mine); ++k) mbar_wait(&s_full[warp][k % QR_STAGES], (k / QR_STAGES) & 1, &s_late);
+      break;
+    }
     issue(i + QR_STAGES, paged && lane < 4 ? s_page[warp][(i + QR_STAGES) & 3][lane & 1] : 0);
   }
   asm volatile("cp.async.wait_group 0;\n" ::: "memory");

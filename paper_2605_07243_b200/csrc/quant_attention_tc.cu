@@ -404,6 +404,13 @@ __device__ inline bool quant_unit_of_rank(const QuantAttnParams& p, int most, in
   return b >= 0;
 }
 
+// After a wait that gave up: shared memory must not be given back under copies in flight.  The last one of every stage is awaited, again with
+// a limit.
+static __device__ __noinline__ void await_loads(uint64_t* bars, const int* asked, int first_k, volatile int* abort_flag) {
+  for (int k = max(first_k, asked[0] - 3); k < asked[0]; ++k) mbar_wait(&bars[QB_K_FULL0 + k % 3], (k / 3) & 1, abort_flag);
+  for (int k = max(0, asked[1] - 3); k < asked[1]; ++k) mbar_wait(&bars[QB_VR_FULL0 + k % 3], (k / 3) & 1, abort_flag);
+}
+
 template <int D>
 __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttnParams p, const __grid_constant__ CUtensorMap kmap,
                                                                  const __grid_constant__ CUtensorMap vmap, const int box_rows) {
@@ -418,6 +425,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
   uint32_t* s_tmem = reinterpret_cast<uint32_t*>(base + 3328);
   volatile int* s_abort = reinterpret_cast<volatile int*>(base + 3332);   // [0] a wait gave up; [1] the same for the last wait
   int* s_err = reinterpret_cast<int*>(base + 3340);
+  int* s_asked = reinterpret_cast<int*>(base + 3392);                // blocks of K and of V codes that the loader has asked for
   uint32_t* s_bad = reinterpret_cast<uint32_t*>(base + 3344);        // [4]: node rows with a NaN or an infinity
   uint32_t* s_flag = reinterpret_cast<uint32_t*>(base + 3360);       // [8 slots]: bits 0-7 the groups with a NaN scale, bits 8-15 those whose V reads as zeros
   // Eight slots: the loader writes block j's when S of block j - 3 is done, i.e. the softmax with block j - 5.
@@ -775,6 +783,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       return __ldg(table + (my_key(j) >> page_shift));
     };
     int page = my_page(tree_blocks);
+    int asked_k = tree_blocks, asked_v = 0;  // blocks asked for
     for (int j = tree_blocks; j < nb; ++j) {
       const int r = j - tree_blocks;                            // the stages of V codes are used from the first prefix block on
       const int key = my_key(j);
@@ -798,12 +807,14 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       if (lane == 0) mbar_expect_tx(&s_bar[QB_K_FULL0 + ks_at], pieces * box_rows * D);
       __syncwarp();
       if (piece) tma_load_4d(smem_u32(sK) + ks_at * TILE8 + 16 * lane * D, &kmap, 0, g, c2, c3, &s_bar[QB_K_FULL0 + ks_at]);
+      asked_k = j + 1;
       if (r >= 3) ok = ok && mbar_wait(&s_bar[QB_VR_EMPTY0 + vs_at], (r / 3 - 1) & 1, s_abort);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) break;
       if (lane == 0) mbar_expect_tx(&s_bar[QB_VR_FULL0 + vs_at], pieces * box_rows * D);
       __syncwarp();
       if (piece) tma_load_4d(smem_u32(sVr) + vs_at * TILE8 + 16 * lane * D, &vmap, 0, g, c2, c3, &s_bar[QB_VR_FULL0 + vs_at]);
+      asked_v = r + 1;
       // A NaN scale poisons the rows that see one of its keys; it is noted, and 1 takes its place, so that it meets no other row.
       const uint32_t nan = __ballot_sync(0xffffffffu, ks != ks || vs != vs), tiny = __ballot_sync(0xffffffffu, vs < kMinVScale);
       if (ks != ks || vs != vs) ks = vs = 1.f;
@@ -817,6 +828,10 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       if (lane == 0) s_flag[j & 7] = nan | (tiny << 8);
       __syncwarp();
       if (lane == 0) mbar_arrive(&s_bar[QB_SC0 + (j & 7)]);
+    }
+    if (lane == 0) {
+      s_asked[0] = asked_k;
+      s_asked[1] = asked_v;
     }
     if (!ok && lane == 0) atomicMax(&p.status[b], (int)SB_ERR_CUDA);
   } else {
@@ -990,6 +1005,7 @@ __global__ void __launch_bounds__(QT_THREADS, 1) quant_tc_kernel(const QuantAttn
       }
     }
   }
+  if (warp == QT_LOAD_WARP && s_abort[0]) await_loads(s_bar, s_asked, tree_blocks, s_abort + 1);
 }
 
 template <int D>
