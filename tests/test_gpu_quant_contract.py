@@ -189,3 +189,80 @@ def test_attention_serves_its_rows_beside_others_with_any_number_of_chunks(P, N,
                                q_offsets=i32([0, N[0]]))
     assert (out[total:] == 3.0).all() and (lse[total:] == 3.0).all()
     assert torch.equal(out[:total], want) and torch.equal(lse[:total], wlse)
+
+
+# ---- together -------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_a_step_of_all_calls_replays_from_a_graph(n):
+    """Fork, reserve, copy, attend, append, release and compact as one graph: replayed from the same state it leaves, bit for bit, what the
+    calls leave one by one; replayed on other inputs, what they leave on those."""
+    H, G, D, ps, block, slots, num, layers = 4, 4, 64, 32, 16, 6, 60, 2
+    rng = np.random.default_rng(76)
+    pool = sb.PagePool.empty(slots, 10, num, ps)
+    codes = [torch.zeros(layers, num, ps, H, D, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    scales = [torch.ones(layers, num, ps // block, H, device="cuda") for _ in range(2)]
+    kv = sb.QuantCache(codes[0], codes[1], scales[0], scales[1], H, D, block, page_size=ps, page_table=pool.page_table, n_layers=layers)
+    arrays = sb.PageArrays(codes + scales, n_layers=layers, num_pages=num)
+    copies = [sb.PageCopies.empty(num) for _ in range(2)]
+    length = i32([0] * slots)
+    # a prompt in slots 0 and 1
+    sb.sb_pages_reserve(pool, i32([0, 1]), i32([0, 0]), i32([100, 75]), copies[0])
+    rows = [qh.bf16_of(rng.normal(size=(layers, 175, H, D))).cuda() for _ in range(2)]
+    new, status = sb.sb_kv_append_quant(kv, rows[0], rows[1], i32([0, 100, 175, 175, 175, 175, 175]), length, max_rows=100)
+    assert status.tolist() == [0] * slots
+    length = i32([100, 75, 75, 0, 0, 0])             # slot 2 will branch from slot 1
+    offs, live = i32([n * b for b in range(slots + 1)]), i32([0, 1, 2])
+    parents = [qh.random_parents(rng, n) for _ in range(slots)]
+    q, k, v = (qh.bf16_of(rng.normal(size=(n * slots, h, D))).cuda() for h in (H * G, H, H))
+    kl, vl = (torch.stack([x, x * 0.5]) for x in (k, v))
+    path = i32([sorted(qh.chain(t, n - 1))[:4] + [-1] * (4 - min(4, len(qh.chain(t, n - 1)))) for t in parents])
+    accept = (path >= 0).sum(dim=1, dtype=torch.int32) - 1
+    tree = sb.QuantTree(n_q_heads=H * G, prefix_len=length, node_offsets=offs, parent=i32([p for t in parents for p in t]), max_nodes=n, max_prefix=200)
+    slots_of = [i32([1]), i32([2]), i32([75])]
+    grown = i32([104, 79, 79])
+    gone, none = i32([0]), i32([0])
+    state = [pool.page_table, pool.held, pool.refs] + codes + scales
+    start = [t.clone() for t in state]
+
+    def step():
+        out = [sb.sb_pages_fork(pool, *slots_of),
+               sb.sb_pages_reserve(pool, live, length[:3], grown, copies[0])]
+        sb.sb_pages_copy(arrays, copies[0])
+        out += sb.sb_tree_attention_quant(kv, tree, q, k, v, layer=1, window=60, sinks=4, num_splits=2)
+        out += sb.sb_kv_append_quant(kv, kl, vl, offs, length, max_rows=4, path_nodes=path, accept_len=accept, max_depth=3)
+        out += [sb.sb_pages_release(pool, gone, none), sb.sb_pages_compact(pool, copies[1])]
+        sb.sb_pages_copy(arrays, copies[1])
+        return out
+
+    def run(fn):
+        for t, was in zip(state, start):
+            t.copy_(was)
+        out = fn()
+        torch.cuda.synchronize()
+        return [t.clone() for t in state + list(out) + [copies[1].src, copies[1].dst]]
+
+    want = run(step)
+    assert want[len(state)].tolist() == [0] and want[len(state) + 1].tolist() == [0, 0, 0]
+    assert want[len(state) + 4].tolist()[:3] == [0, 0, 0] and want[len(state) + 6].tolist()[:3] == [0, 0, 0]
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            held = step()
+    torch.cuda.current_stream().wait_stream(side)
+
+    def replay():
+        g.replay()
+        return held
+
+    for _ in range(5):
+        for a, b in zip(run(replay), want):
+            assert torch.equal(a, b)
+    q.mul_(0.5)
+    kl.neg_()
+    k.copy_(kl[0])
+    want = run(step)
+    for a, b in zip(run(replay), want):
+        assert torch.equal(a, b)
